@@ -28,6 +28,11 @@
  *                               (Sec. 3.3, region-guided latent reuse and
  *                               joint reuse in intermediate layers; Appendix
  *                               C.3)
+ *   carnator_page_plan, carnator_kv4_store, carnator_kv4_load,
+ *   carnator_kv4_attn           cached K and V of a request, held in 4 bits
+ *                               in pages of one block, and attention over
+ *                               them (Sec. 3.3, cached computation of the
+ *                               tokens outside the active region)
  *   carnator_ciede2000, carnator_shape_descriptor,
  *   carnator_object_discrepancy, carnator_compat_gate,
  *   carnator_clopper_pearson_upper
@@ -89,7 +94,7 @@
 extern "C" {
 #endif
 
-#define CARNATOR_ABI_VERSION 7
+#define CARNATOR_ABI_VERSION 8
 
 typedef enum {
   CARNATOR_OK = 0,
@@ -256,6 +261,132 @@ int carnator_block_mass_exact(const carnator_view *q_hist, const carnator_view *
 int carnator_select_block_mask(const double *mass, const carnator_shape *shape,
                                double mass_threshold, uint8_t *mask_out, uint64_t *bits_out,
                                hipStream_t stream);
+
+/*
+ * Cached keys and values held in 4 bits -- Sec. 3.3: tokens outside the
+ * active region keep their cached computation.  Their K and V are kept in
+ * pages of `block` tokens; a table names the pages of each request, so
+ * requests share pages and a page can be left out.  The same calls serve a
+ * model that generates token by token or frame by frame: K and V of the new
+ * tokens are appended, and their queries attend to what is cached.
+ *
+ * Format.  32 channels of a token share a scale 2^e; a value is a sign and one
+ * of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 to 7, the sign is bit 3) times the
+ * scale.  e is the least integer in [-125, 125] for which no magnitude of the
+ * group exceeds 7 * 2^e: then every value is off by half a step of its
+ * neighbours at most (6 is the nearest level up to 7).  Values are rounded to
+ * the nearest level, ties to the even code; magnitudes above 7 * 2^125 saturate
+ * at 6 * 2^125.  The scale is stored as the byte e + 127; 255 marks a group
+ * that held an infinity or NaN and reads back as NaN throughout.  17 / 32 of a
+ * byte a value.
+ *
+ * Page p holds, for each of the kv_heads heads in turn,
+ *   K codes   uint8 [block][d / 2]: channel 2i in the low half of byte i,
+ *             2i + 1 in the high half
+ *   K scales  uint8 [block][d / 32]
+ *   V codes   uint8 [block / 8][d / 2][8]: the same bytes, those of eight
+ *             consecutive tokens side by side
+ *   V scales  uint8 [block / 8][d / 32][8]
+ * block * d * 17 / 16 bytes a head, carnator_kv4_page_bytes a page (0 if the
+ * sizes are not supported).  Slot s is token s mod block of page s / block.
+ *
+ * carnator_kv4: pages 16-byte aligned, n_pages * block <= 2^31 - 1.
+ * carnator_rows: a bf16 [rows, heads, d] tensor, d contiguous, element strides
+ * (multiples of 8), data 16-byte aligned.
+ * Tables are int32 [batch][width]: entry j is the page of tokens [j * block,
+ * (j + 1) * block) of a request; an entry outside [0, n_pages) is no page, and
+ * its tokens are left out.  kv_len int32 [batch]: tokens of each request, read
+ * as clamped into [0, width * block]; width * block <= 2^30.
+ *
+ * carnator_page_plan: where the new tokens of each request go.  With P = block,
+ * n_b = new_len[b] (0 if negative; cut where the sum over b passes n_slots),
+ * full_b = ceil(kv_b / P), want_b = min(width, ceil((kv_b + n_b) / P)) - full_b
+ * and first_b the sum of want over the requests before b: page full_b + i of
+ * request b, i < want_b, is free_pages[first_b + i] (none from n_free on).
+ *   kv_len      int32 [batch], tokens held before
+ *   new_len     int32 [batch]
+ *   table       int32 [batch][width], the new pages are written; the other
+ *               entries are left as they are
+ *   free_pages  int32 [n_free] (may be NULL if n_free is 0)
+ *   q_start     int32 [batch + 1] out: sums of n, starting with 0
+ *   kv_len_out  int32 [batch] out: kv_b + placed_b, placed_b the new tokens
+ *               with an entry in the table and a page from the list (the
+ *               first ones of n_b).  Not kv_len itself.
+ *   slots       int32 [n_slots] out: of new token i of request b at
+ *               q_start[b] + i, in the page of position kv_b + i; -1 without a
+ *               page, and behind the last token
+ *   positions   int32 [n_slots] out or NULL: kv_b + i; -1 behind the last token
+ *   counts      int32 [3] out: the tokens (q_start[batch]), the pages taken
+ *               from the list, and the tokens of new_len that were not placed
+ *               (at most 2^31 - 1)
+ * batch <= 16384.  table, slots and the other outputs must not overlap.
+ * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED, E_ALIGN, E_HIP.
+ *
+ * carnator_kv4_store: quantises row r of k and v into slot slots[r]; rows with
+ * a slot outside [0, n_pages * block) are skipped.  A slot may occur once.
+ * Nothing else of a page is written.  n_rows may be 0.
+ * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED, E_ALIGN, E_HIP.
+ *
+ * carnator_kv4_load: the first kv_len tokens of each request, at most n, as
+ * bf16 (exact: a level times a power of two).
+ *   k_out, v_out  bf16 [batch, kv_heads, n, d] at element strides b, h, n
+ *                 (multiples of 8, d contiguous); rows past a request's length
+ *                 or without a page are left untouched
+ * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED, E_ALIGN, E_HIP.
+ *
+ * carnator_kv4_attn: for query row t = q_start[b] + i of request b, m_b =
+ * q_start[b + 1] - q_start[b], and head h reading cached head
+ * h / (heads / kv_heads), with A the tokens j < kv_b that have a page and, if
+ * causal, j <= kv_b - m_b + i:
+ *   o = sum_{j in A} softmax_j(sigma q . k_j) v_j,
+ *   lse = log sum_{j in A} exp(sigma q . k_j),
+ * sigma = scale, or 1/sqrt(head_dim) when scale <= 0.  No token in A gives
+ * o = 0 and lse = -inf.  bf16 matrix cores, fp32 accumulation and softmax; O
+ * is rounded to bf16.  A value outside A has no effect, be it NaN.
+ *   q           bf16 [n_rows, heads, d]
+ *   q_start     int32 [batch + 1], ascending, read as clamped into [0, n_rows]
+ *   max_q       at least every m_b (>= 1); rows of a request from max_q on are
+ *               left out
+ *   out         bf16 [n_rows, heads, d] at element strides; rows before
+ *               q_start[0] and behind q_start[batch] are left untouched; may
+ *               not alias q or the pages
+ *   lse         fp32 [n_rows, heads] contiguous, or NULL
+ *   workspace   carnator_kv4_attn_workspace_size bytes, 256-byte aligned
+ * heads a multiple of kv_heads; n_rows may be 0.
+ * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED, E_ALIGN, E_WORKSPACE, E_HIP.
+ */
+typedef struct {
+  void *pages;
+  int32_t n_pages;
+  int32_t kv_heads;
+  int32_t head_dim; /* 64 or 128 */
+  int32_t block;    /* 64 or 128 */
+} carnator_kv4;
+
+typedef struct {
+  const void *data;
+  int64_t stride_t;
+  int64_t stride_h;
+} carnator_rows;
+
+int64_t carnator_kv4_page_bytes(int32_t kv_heads, int32_t head_dim, int32_t block);
+int carnator_page_plan(const int32_t *kv_len, const int32_t *new_len, int32_t batch, int32_t *table,
+                       int32_t width, const int32_t *free_pages, int32_t n_free, int32_t block,
+                       int32_t *q_start, int32_t *kv_len_out, int32_t *slots, int32_t *positions,
+                       int32_t n_slots, int32_t *counts, hipStream_t stream);
+int carnator_kv4_store(const carnator_kv4 *cache, const carnator_rows *k, const carnator_rows *v,
+                       int32_t n_rows, const int32_t *slots, hipStream_t stream);
+int carnator_kv4_load(const carnator_kv4 *cache, const int32_t *table, int32_t batch, int32_t width,
+                      const int32_t *kv_len, int32_t n, void *k_out, int64_t k_stride_b,
+                      int64_t k_stride_h, int64_t k_stride_n, void *v_out, int64_t v_stride_b,
+                      int64_t v_stride_h, int64_t v_stride_n, hipStream_t stream);
+size_t carnator_kv4_attn_workspace_size(const carnator_kv4 *cache, int32_t heads, int32_t n_rows,
+                                        int32_t batch, int32_t width, int32_t max_q);
+int carnator_kv4_attn(const carnator_rows *q, int32_t n_rows, int32_t heads,
+                      const carnator_kv4 *cache, const int32_t *table, int32_t batch, int32_t width,
+                      const int32_t *q_start, const int32_t *kv_len, int32_t max_q, int32_t causal,
+                      float scale, void *out, int64_t out_stride_t, int64_t out_stride_h, float *lse,
+                      void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
  * Compatibility gate -- Sec. 3.2 ("Reuse Validity with Generation-Native

@@ -38,6 +38,11 @@ Every function is plain fp64 NumPy, written from the paper's definitions:
   signature against a bank of cached signatures (Sec. 3.1 problem setup,
   Sec. 4.1 "Candidate Recall").
 
+* ``kv4_quantise`` / ``kv4_values`` / ``kv4_store`` / ``kv4_token`` /
+  ``kv4_cached`` / ``kv4_attention`` / ``page_plan``: cached keys and values in
+  4 bits, their pages and the attention over them (Sec. 3.3: tokens outside the
+  active region keep their cached computation).
+
 Readings taken where the paper is silent are listed in the module docstrings
 of each submodule.
 """
@@ -51,6 +56,7 @@ from .exact_mass import exact_block_mass, select_row_mass, mask_from_mass, row_a
 from .region import (dilate_frames, chebyshev_distance, smoothstep, regions, latent_fusion,
                      region_block_flags, restrict_mask, compact_restricted)
 from .cosine import cosine_similarity, topk_cosine
+from .kv4 import (kv4_quantise, kv4_values, kv4_store, kv4_token, kv4_cached, kv4_attention, page_plan)
 from .convert import to_f64
 
 __all__ = [
@@ -63,4 +69,5 @@ __all__ = [
     "exact_block_mass", "select_row_mass", "mask_from_mass", "row_admissible_masks_mass",
     "ciede2000", "support_area", "normalized_shape", "d_size", "d_shape", "gate", "first_compatible",
     "clopper_pearson_upper", "SHAPE_RES",
+    "kv4_quantise", "kv4_values", "kv4_store", "kv4_token", "kv4_cached", "kv4_attention", "page_plan",
 ]

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_PKG, "libcarnator.so")
 
 CARNATOR_OK = 0
 # CARNATOR_ABI_VERSION of include/carnator.h this binding marshals for
-ABI_VERSION = 7
+ABI_VERSION = 8
 STATUS = {0: "OK", -1: "E_NULL", -2: "E_SHAPE", -3: "E_UNSUPPORTED", -4: "E_ALIGN",
           -5: "E_WORKSPACE", -6: "E_HIP"}
 
@@ -35,6 +35,8 @@ EXPORTS = (
     "carnator_region_weights_workspace_size", "carnator_region_weights", "carnator_latent_fusion",
     "carnator_region_block_flags", "carnator_compact_block_mask_bits_region",
     "carnator_block_sparse_attn_rows",
+    "carnator_kv4_page_bytes", "carnator_page_plan", "carnator_kv4_store", "carnator_kv4_load",
+    "carnator_kv4_attn_workspace_size", "carnator_kv4_attn",
     "carnator_block_sparse_attn_workspace_size", "carnator_block_sparse_attn",
     "carnator_block_sparse_attn_lists",
     "carnator_signature_sim_workspace_size", "carnator_signature_sim", "carnator_signature_sim_noalloc",
@@ -51,6 +53,15 @@ class Shape(ctypes.Structure):
 class View(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
                 ("stride_n", ctypes.c_int64)]
+
+
+class Kv4(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
 
 
 class CarnatorError(RuntimeError):
@@ -72,6 +83,7 @@ def lib() -> ctypes.CDLL:
         P, I32, I64, SZ, F32, F64 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t,
                                      ctypes.c_float, ctypes.c_double)
         SP, VP = ctypes.POINTER(Shape), ctypes.POINTER(View)
+        CP, RP = ctypes.POINTER(Kv4), ctypes.POINTER(Rows)
         sig = {
             "carnator_abi_version": (ctypes.c_int, []),
             "carnator_order_group_heads": (ctypes.c_int32, [ctypes.POINTER(Shape)]),
@@ -102,6 +114,13 @@ def lib() -> ctypes.CDLL:
                                                           SZ, P]),
             "carnator_block_sparse_attn_lists": (ctypes.c_int, [VP, VP, VP, P, I64, I64, I64, SP, P, P, P, F32,
                                                                 P, P]),
+            "carnator_kv4_page_bytes": (I64, [I32, I32, I32]),
+            "carnator_page_plan": (ctypes.c_int, [P, P, I32, P, I32, P, I32, I32, P, P, P, P, I32, P, P]),
+            "carnator_kv4_store": (ctypes.c_int, [CP, RP, RP, I32, P, P]),
+            "carnator_kv4_load": (ctypes.c_int, [CP, P, I32, I32, P, I32, P, I64, I64, I64, P, I64, I64, I64, P]),
+            "carnator_kv4_attn_workspace_size": (SZ, [CP, I32, I32, I32, I32, I32]),
+            "carnator_kv4_attn": (ctypes.c_int, [RP, I32, I32, CP, P, I32, I32, P, P, I32, I32, F32, P, I64, I64, P,
+                                                 P, SZ, P]),
             "carnator_signature_sim_workspace_size": (SZ, [I64, I64, I32]),
             "carnator_signature_sim": (ctypes.c_int, [P, I64, P, I64, I64, I64, I32, P, P, P, P, SZ, P]),
             "carnator_signature_sim_noalloc": (ctypes.c_int, [P, I64, P, I64, I64, I64, I32, P, P, P, P]),
@@ -620,6 +639,232 @@ def compact_block_mask_bits_region(bits: torch.Tensor, active_q, context_k, out=
                                                          _ptr(row_ptr), _ptr(col_idx), _ptr(order), _ptr(n_active),
                                                          _ptr(workspace), workspace.numel(), _stream(bits)))
     return row_ptr, col_idx, order, n_active
+
+
+# ---------------------------------------------------------------- 4-bit cached keys and values
+#
+# A pool is a uint8 tensor [n_pages, kv_heads, block * d * 17 / 16] holding the
+# pages of include/carnator.h, a table int32 [batch, width] names the pages of
+# each request (-1: none), a slot is page * block + token.
+
+def kv4_pool(n_pages: int, kv_heads: int, head_dim: int, block: int, device="cuda") -> torch.Tensor:
+    """An empty pool of pages for kv_heads heads of head_dim channels."""
+    if lib().carnator_kv4_page_bytes(int(kv_heads), int(head_dim), int(block)) <= 0:
+        raise ValueError("kv_heads must be 1 to 65535, head_dim and block 64 or 128")
+    return torch.zeros(n_pages, kv_heads, block * head_dim * 17 // 16, dtype=torch.uint8, device=device)
+
+
+def _kv4(pool: torch.Tensor, block: int) -> Kv4:
+    if pool.dim() != 3 or pool.dtype != torch.uint8 or not pool.is_cuda or not pool.is_contiguous():
+        raise ValueError("pool must be a contiguous uint8 CUDA tensor [n_pages, kv_heads, block * d * 17 / 16]")
+    n_pages, heads, size = pool.shape
+    d = size * 16 // (17 * block)
+    if block * d * 17 // 16 != size:
+        raise ValueError("the pool's pages hold %d bytes a head, no multiple of 17 / 16 of block %d" % (size, block))
+    return Kv4(pool.data_ptr(), n_pages, heads, d, block)
+
+
+def _rows(t: torch.Tensor, name: str, heads: int, d: int, device) -> Rows:
+    if t.dim() != 3 or t.dtype != torch.bfloat16 or t.device != device or t.shape[1] != heads or t.shape[2] != d:
+        raise ValueError("%s must be a bf16 tensor [rows, %d, %d] on %s" % (name, heads, d, device))
+    st, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError("%s must be contiguous along its channels" % name)
+    return Rows(t.data_ptr(), st, sh)
+
+
+def _i32(t: torch.Tensor, name: str, shape, device) -> int:
+    if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor %s on %s" % (name, list(shape), device))
+    return t.data_ptr()
+
+
+def _call(f, device, *args):
+    """A library call with its device as the current one."""
+    index = device.index
+    if torch._C._cuda_getDevice() == index:
+        _check(f(*args, torch._C._cuda_getCurrentRawStream(index)))
+    else:
+        with torch.cuda.device(index):
+            _check(f(*args, torch._C._cuda_getCurrentRawStream(index)))
+
+
+def page_plan(kv_len: torch.Tensor, new_len: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor, block: int,
+              n_slots: int, out=None):
+    """Where the new tokens of each request go (carnator_page_plan): new pages
+    are taken from free_pages in order and entered in ``table`` (in place).
+
+    kv_len, new_len int32 [batch]; table int32 [batch, width]; n_slots the
+    capacity of the batch in tokens (at least the sum of new_len, or the rest
+    is not placed).  Returns int32 (q_start [batch + 1], kv_len_out [batch],
+    slots [n_slots], positions [n_slots], counts [3]); ``out`` may pass them
+    preallocated (positions may be None).  Nothing synchronises.
+    """
+    if not kv_len.is_cuda:
+        raise ValueError("kv_len must be a CUDA tensor")
+    dev = kv_len.device
+    if kv_len.dim() != 1 or table.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError("expected kv_len [batch], table [batch, width] and free_pages [n]")
+    B, W = kv_len.shape[0], table.shape[1]
+    n_slots = int(n_slots)
+    if out is None:
+        if n_slots < 0:
+            raise ValueError("n_slots must be >= 0")
+        out = [torch.empty(n, dtype=torch.int32, device=dev) for n in (B + 1, B, n_slots, n_slots, 3)]
+    q_start, kv_out, slots, positions, counts = out
+    _call(lib().carnator_page_plan, dev, _i32(kv_len, "kv_len", (B,), dev), _i32(new_len, "new_len", (B,), dev), B,
+          _i32(table, "table", (B, W), dev), W, _i32(free_pages, "free_pages", (free_pages.shape[0],), dev),
+          free_pages.shape[0], int(block), _i32(q_start, "q_start", (B + 1,), dev),
+          _i32(kv_out, "kv_len_out", (B,), dev), _i32(slots, "slots", (n_slots,), dev),
+          None if positions is None else _i32(positions, "positions", (n_slots,), dev), n_slots,
+          _i32(counts, "counts", (3,), dev))
+    return q_start, kv_out, slots, positions, counts
+
+
+def kv4_store(pool: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, block: int) -> torch.Tensor:
+    """Quantises the rows of k and v (bf16 [rows, kv_heads, d]) into the slots
+    int32 [rows] of the pool, in place (carnator_kv4_store); rows with a slot of
+    -1 are skipped.  Returns ``pool``."""
+    c = _kv4(pool, block)
+    dev = pool.device
+    kr, vr = _rows(k, "k", c.kv_heads, c.head_dim, dev), _rows(v, "v", c.kv_heads, c.head_dim, dev)
+    if v.shape[0] != k.shape[0]:
+        raise ValueError("k and v have %d and %d rows" % (k.shape[0], v.shape[0]))
+    _call(lib().carnator_kv4_store, dev, ctypes.byref(c), ctypes.byref(kr), ctypes.byref(vr), k.shape[0],
+          _i32(slots, "slots", (k.shape[0],), dev))
+    return pool
+
+
+def kv4_load(pool: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, block: int, n: Optional[int] = None,
+             out=None):
+    """(k, v) bf16 [batch, kv_heads, n, d]: the first kv_len tokens of each
+    request (carnator_kv4_load), n = width * block if None.  ``out`` may pass
+    (k, v) of any strides with d contiguous, whose other rows (past a request's
+    length, or without a page) stay as they are; without it they are 0."""
+    c = _kv4(pool, block)
+    dev = pool.device
+    if table.dim() != 2:
+        raise ValueError("table must be [batch, width]")
+    B, W = table.shape
+    if out is None:
+        n = W * block if n is None else int(n)
+        out = tuple(torch.zeros(B, c.kv_heads, n, c.head_dim, dtype=torch.bfloat16, device=dev) for _ in range(2))
+    k, v = out
+    n = k.shape[2] if n is None and k.dim() == 4 else n
+    for t, name in ((k, "k"), (v, "v")):
+        if (tuple(t.shape) != (B, c.kv_heads, n, c.head_dim) or t.dtype != torch.bfloat16 or t.device != dev
+                or t.stride(3) != 1):
+            raise ValueError("%s must be a bf16 tensor %s on %s, contiguous along its channels"
+                             % (name, [B, c.kv_heads, n, c.head_dim], dev))
+    ks, vs = k.stride(), v.stride()
+    _call(lib().carnator_kv4_load, dev, ctypes.byref(c), _i32(table, "table", (B, W), dev), B, W,
+          _i32(kv_len, "kv_len", (B,), dev), n, k.data_ptr(), ks[0], ks[1], ks[2], v.data_ptr(), vs[0], vs[1], vs[2])
+    return k, v
+
+
+def kv4_attn_workspace(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, max_q: int, block: int) -> torch.Tensor:
+    c = _kv4(pool, block)
+    return _workspace(lib().carnator_kv4_attn_workspace_size(ctypes.byref(c), q.shape[1], q.shape[0], table.shape[0],
+                                                             table.shape[1], int(max_q)), pool.device)
+
+
+def kv4_attn(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+             max_q: int, block: int, causal: bool = False, scale: float = 0.0, return_lse: bool = False,
+             out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+             workspace: Optional[torch.Tensor] = None):
+    """Attention of each request's queries over its cached tokens
+    (carnator_kv4_attn).
+
+    q bf16 [rows, heads, d], heads a multiple of the pool's; rows q_start[b] to
+    q_start[b + 1] (int32 [batch + 1]) belong to request b, at most max_q of
+    them; with ``causal`` they are the last of its kv_len tokens.  Rows of no
+    request stay as they are in ``out`` and ``lse`` (fp32 [rows, heads]) and are
+    0 where the call allocates them.  Returns O (and the LSE)."""
+    c = _kv4(pool, block)
+    dev = pool.device
+    if q.dim() != 3 or table.dim() != 2:
+        raise ValueError("expected q [rows, heads, d] and table [batch, width]")
+    T, heads = q.shape[0], q.shape[1]
+    B, W = table.shape
+    qr = _rows(q, "q", heads, c.head_dim, dev)
+    if out is None:
+        out = torch.zeros(T, heads, c.head_dim, dtype=torch.bfloat16, device=dev)
+    else:
+        _rows(out, "out", heads, c.head_dim, dev)
+        if out.shape[0] != T:
+            raise ValueError("out has %d rows, q %d" % (out.shape[0], T))
+    if not return_lse:
+        lse = None
+    elif lse is None:
+        lse = torch.zeros(T, heads, dtype=torch.float32, device=dev)
+    elif lse.dtype != torch.float32 or lse.device != dev or tuple(lse.shape) != (T, heads) or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous fp32 tensor [rows, heads] on the pool's device")
+    L = lib()
+    if workspace is None:
+        need = L.carnator_kv4_attn_workspace_size(ctypes.byref(c), heads, T, B, W, int(max_q))
+        ws, size = (_workspace(need, dev), need) if need else (None, 0)
+    else:
+        ws, size = workspace, workspace.numel()
+    _call(L.carnator_kv4_attn, dev, ctypes.byref(qr), T, heads, ctypes.byref(c), _i32(table, "table", (B, W), dev), B, W,
+          _i32(q_start, "q_start", (B + 1,), dev), _i32(kv_len, "kv_len", (B,), dev), int(max_q), int(bool(causal)),
+          float(scale), out.data_ptr(), out.stride(0), out.stride(1), _ptr(lse), _ptr(ws), size)
+    return (out, lse) if return_lse else out
+
+
+class Kv4Cache:
+    """The cached keys and values of a batch of requests in 4 bits: a pool of
+    pages, the table and the length of each request, and the pages that are
+    free, all on the device.  A page may be named by several requests' tables
+    (a target that keeps the history's pages for the blocks it does not
+    recompute); a table entry of -1 leaves its block out."""
+
+    def __init__(self, n_pages: int, batch: int, width: int, kv_heads: int, head_dim: int, block: int, device="cuda"):
+        self.block = block
+        self.pool = kv4_pool(n_pages, kv_heads, head_dim, block, device)
+        device = self.pool.device
+        self.table = torch.full((batch, width), -1, dtype=torch.int32, device=device)
+        self.kv_len = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.free = torch.arange(n_pages, dtype=torch.int32, device=device)
+
+    @property
+    def nbytes(self) -> int:
+        return self.pool.numel()
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, new_len: torch.Tensor):
+        """Appends the rows of k and v (bf16 [rows, kv_heads, d]), new_len[b]
+        of them to request b in turn, and drops the pages they take from the
+        free list, for which the stream is synchronised once (page_plan and
+        kv4_store do not).  Returns (q_start, positions, lacking): the rows'
+        starts and positions, and the number of tokens without a page or an
+        entry in the table, which are not held."""
+        q_start, kv_len, slots, positions, counts = page_plan(self.kv_len, new_len, self.table, self.free, self.block,
+                                                              k.shape[0])
+        kv4_store(self.pool, k, v, slots, self.block)
+        self.kv_len = kv_len
+        _, taken, lacking = counts.tolist()
+        self.free = self.free[taken:]
+        return q_start, positions, lacking
+
+    def release(self, requests) -> None:
+        """Empties the requests (indices); their pages that no other table row
+        names are free again."""
+        pages = self.table[requests].flatten()
+        self.table[requests] = -1
+        self.kv_len[requests] = 0
+        pages = pages[pages >= 0].unique()
+        self.free = torch.cat([self.free, pages[~torch.isin(pages, self.table)]])
+
+    def load(self, n: Optional[int] = None, out=None, keep=None):
+        """kv4_load of every request; ``keep`` (uint8 [batch, width], as the
+        context flags of region_block_flags) leaves the other blocks out."""
+        return kv4_load(self.pool, self._kept(keep), self.kv_len, self.block, n, out)
+
+    def attn(self, q: torch.Tensor, q_start: torch.Tensor, max_q: int, keep=None, **kw):
+        """kv4_attn over every request (keep as in load)."""
+        return kv4_attn(q, self.pool, self._kept(keep), q_start, self.kv_len, max_q, self.block, **kw)
+
+    def _kept(self, keep) -> torch.Tensor:
+        return self.table if keep is None else self.table.masked_fill(keep == 0, -1)
 
 
 def signature_sim_workspace(nq: int, m: int, topk: int, device) -> torch.Tensor:

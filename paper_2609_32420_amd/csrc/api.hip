@@ -9,6 +9,8 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <initializer_list>
+
 using namespace carnator;
 
 namespace {
@@ -522,6 +524,211 @@ int carnator_block_sparse_attn_rows(const carnator_view *q, const carnator_view 
   if (!n_rows) return fail(CARNATOR_E_NULL, "n_rows is NULL");
   return attn_lists(q, k, v, out, osb, osh, osn, s, row_ptr, col_idx, order, n_rows, scale, lse,
                     stream);
+}
+
+// ---------------------------------------------------------------- 4-bit cached keys and values
+
+namespace {
+
+// Tokens of a table's width, and threads of a launch (a HIP grid holds 2^32).
+constexpr int64_t kMaxReach = (int64_t)1 << 30;
+constexpr int64_t kMaxWorkgroups = ((int64_t)1 << 24) - 1;
+
+int check_block(int32_t block) {
+  if (block != 64 && block != 128)
+    return fail(CARNATOR_E_UNSUPPORTED, "block must be 64 or 128 (got %d)", block);
+  return CARNATOR_OK;
+}
+
+int check_kv4(const carnator_kv4 *c) {
+  int rc;
+  if (!c || !c->pages) return fail(CARNATOR_E_NULL, "the cache or its pages are NULL");
+  if (c->n_pages < 1 || c->kv_heads < 1)
+    return fail(CARNATOR_E_SHAPE, "n_pages and kv_heads must be >= 1 (got %d, %d)", c->n_pages, c->kv_heads);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(CARNATOR_E_UNSUPPORTED, "head_dim must be 64 or 128 (got %d)", c->head_dim);
+  if ((rc = check_block(c->block))) return rc;
+  if ((int64_t)c->n_pages * c->block > (int64_t)INT32_MAX)
+    return fail(CARNATOR_E_SHAPE, "n_pages * block exceeds 2^31-1");
+  if (c->kv_heads > 65535) return fail(CARNATOR_E_UNSUPPORTED, "at most 65535 kv_heads");
+  if (reinterpret_cast<uintptr_t>(c->pages) % 16 != 0)
+    return fail(CARNATOR_E_ALIGN, "pages must be 16-byte aligned");
+  return CARNATOR_OK;
+}
+
+int check_rows(const carnator_rows *r, const char *name) {
+  if (!r || !r->data) return fail(CARNATOR_E_NULL, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(r->data) % 16 != 0)
+    return fail(CARNATOR_E_ALIGN, "%s data must be 16-byte aligned", name);
+  if (r->stride_t % 8 || r->stride_h % 8)
+    return fail(CARNATOR_E_ALIGN, "%s strides must be multiples of 8 elements", name);
+  if (r->stride_t < 0 || r->stride_h < 0)
+    return fail(CARNATOR_E_SHAPE, "%s strides must be >= 0", name);
+  return CARNATOR_OK;
+}
+
+// A table of a batch, and the pointers to 4-byte integers beside it.
+int check_table(const int32_t *table, int32_t batch, int32_t width, int32_t block) {
+  if (!table) return fail(CARNATOR_E_NULL, "table is NULL");
+  if (batch < 1 || width < 1)
+    return fail(CARNATOR_E_SHAPE, "batch and width must be >= 1 (got %d, %d)", batch, width);
+  if ((int64_t)width * block > kMaxReach) return fail(CARNATOR_E_SHAPE, "width * block exceeds 2^30");
+  return CARNATOR_OK;
+}
+
+bool misaligned4(std::initializer_list<const void *> ps) {
+  for (const void *p : ps)
+    if (reinterpret_cast<uintptr_t>(p) % 4) return true;
+  return false;
+}
+
+Kv4 to_kv4(const carnator_kv4 *c) {
+  return Kv4{static_cast<unsigned char *>(c->pages), c->n_pages, c->kv_heads, c->head_dim, c->block == 64 ? 6 : 7};
+}
+
+Rows to_rows(const carnator_rows *r) {
+  return Rows{static_cast<const uint16_t *>(r->data), r->stride_t, r->stride_h};
+}
+
+// The sizes of an attention call (pointers apart).
+int check_kv4_attn_sizes(const carnator_kv4 *c, int32_t heads, int32_t n_rows, int32_t batch, int32_t width,
+                         int32_t max_q) {
+  if (heads < 1 || n_rows < 0 || max_q < 1)
+    return fail(CARNATOR_E_SHAPE, "heads and max_q must be >= 1, n_rows >= 0 (got %d, %d, %d)", heads, max_q, n_rows);
+  if (heads % c->kv_heads)
+    return fail(CARNATOR_E_SHAPE, "heads (%d) must be a multiple of kv_heads (%d)", heads, c->kv_heads);
+  if (batch < 1 || width < 1)
+    return fail(CARNATOR_E_SHAPE, "batch and width must be >= 1 (got %d, %d)", batch, width);
+  if ((int64_t)width * c->block > kMaxReach) return fail(CARNATOR_E_SHAPE, "width * block exceeds 2^30");
+  if ((int64_t)n_rows * heads > (int64_t)INT32_MAX)
+    return fail(CARNATOR_E_SHAPE, "n_rows * heads exceeds 2^31-1");
+  return CARNATOR_OK;
+}
+
+Kv4Attn attn_of(const carnator_kv4 *c, int32_t heads, int32_t n_rows, int32_t batch, int32_t width, int32_t max_q) {
+  Kv4Attn a{};
+  a.c = to_kv4(c);
+  a.heads = heads;
+  a.group = heads / c->kv_heads;
+  a.n_rows = n_rows;
+  a.batch = batch;
+  a.width = width;
+  a.max_q = max_q < n_rows ? max_q : n_rows;
+  return a;
+}
+
+}  // namespace
+
+int64_t carnator_kv4_page_bytes(int32_t kv_heads, int32_t head_dim, int32_t block) {
+  if (kv_heads < 1 || kv_heads > 65535 || (head_dim != 64 && head_dim != 128) || (block != 64 && block != 128))
+    return 0;
+  return (int64_t)kv_heads * kv4_head_bytes(head_dim, block);
+}
+
+int carnator_page_plan(const int32_t *kv_len, const int32_t *new_len, int32_t batch, int32_t *table, int32_t width,
+                       const int32_t *free_pages, int32_t n_free, int32_t block, int32_t *q_start,
+                       int32_t *kv_len_out, int32_t *slots, int32_t *positions, int32_t n_slots, int32_t *counts,
+                       hipStream_t stream) {
+  int rc;
+  if ((rc = check_block(block))) return rc;
+  if ((rc = check_table(table, batch, width, block))) return rc;
+  if (batch > kMaxPlanBatch) return fail(CARNATOR_E_UNSUPPORTED, "batch must be at most %d", kMaxPlanBatch);
+  if (n_free < 0 || n_slots < 0) return fail(CARNATOR_E_SHAPE, "n_free and n_slots must be >= 0");
+  if (!kv_len || !new_len || !q_start || !kv_len_out || !counts || (n_free > 0 && !free_pages) ||
+      (n_slots > 0 && !slots))
+    return fail(CARNATOR_E_NULL, "kv_len, new_len, free_pages, q_start, kv_len_out, slots and counts must be non-NULL");
+  if (kv_len_out == kv_len || kv_len_out == new_len)
+    return fail(CARNATOR_E_SHAPE, "kv_len_out must not be kv_len or new_len");
+  if (misaligned4({kv_len, new_len, table, free_pages, q_start, kv_len_out, slots, positions, counts}))
+    return fail(CARNATOR_E_ALIGN, "the arrays must be 4-byte aligned");
+  hipError_t e = launch_page_plan(kv_len, new_len, batch, table, width, free_pages, n_free, block == 64 ? 6 : 7,
+                                  q_start, kv_len_out, slots, positions, n_slots, counts, stream);
+  if (e != hipSuccess) return hip_fail(e, "page_plan");
+  return ok();
+}
+
+int carnator_kv4_store(const carnator_kv4 *cache, const carnator_rows *k, const carnator_rows *v, int32_t n_rows,
+                       const int32_t *slots, hipStream_t stream) {
+  int rc;
+  if ((rc = check_kv4(cache))) return rc;
+  if (n_rows < 0) return fail(CARNATOR_E_SHAPE, "n_rows must be >= 0");
+  if (n_rows == 0) return ok();
+  if ((rc = check_rows(k, "k")) || (rc = check_rows(v, "v"))) return rc;
+  if (!slots) return fail(CARNATOR_E_NULL, "slots is NULL");
+  if (misaligned4({slots})) return fail(CARNATOR_E_ALIGN, "slots must be 4-byte aligned");
+  hipError_t e = launch_kv4_store(to_kv4(cache), to_rows(k), to_rows(v), n_rows, slots, stream);
+  if (e != hipSuccess) return hip_fail(e, "kv4_store");
+  return ok();
+}
+
+int carnator_kv4_load(const carnator_kv4 *cache, const int32_t *table, int32_t batch, int32_t width,
+                      const int32_t *kv_len, int32_t n, void *k_out, int64_t ksb, int64_t ksh, int64_t ksn,
+                      void *v_out, int64_t vsb, int64_t vsh, int64_t vsn, hipStream_t stream) {
+  int rc;
+  if ((rc = check_kv4(cache))) return rc;
+  if ((rc = check_table(table, batch, width, cache->block))) return rc;
+  if (n < 0) return fail(CARNATOR_E_SHAPE, "n must be >= 0");
+  if (n == 0) return ok();
+  if (!kv_len || !k_out || !v_out) return fail(CARNATOR_E_NULL, "kv_len, k_out and v_out must be non-NULL");
+  if (misaligned4({table, kv_len})) return fail(CARNATOR_E_ALIGN, "table and kv_len must be 4-byte aligned");
+  if (reinterpret_cast<uintptr_t>(k_out) % 16 || reinterpret_cast<uintptr_t>(v_out) % 16)
+    return fail(CARNATOR_E_ALIGN, "k_out and v_out must be 16-byte aligned");
+  if (ksb % 8 || ksh % 8 || ksn % 8 || vsb % 8 || vsh % 8 || vsn % 8)
+    return fail(CARNATOR_E_ALIGN, "output strides must be multiples of 8 elements");
+  if (ksn < cache->head_dim || vsn < cache->head_dim || ksb < 0 || ksh < 0 || vsb < 0 || vsh < 0)
+    return fail(CARNATOR_E_SHAPE, "output strides out of range (stride_n >= head_dim, others >= 0)");
+  if ((int64_t)batch * cache->kv_heads > (int64_t)INT32_MAX)
+    return fail(CARNATOR_E_SHAPE, "batch * kv_heads exceeds 2^31-1");
+  hipError_t e = launch_kv4_load(to_kv4(cache), table, batch, width, kv_len, n, static_cast<uint16_t *>(k_out), ksb,
+                                 ksh, ksn, static_cast<uint16_t *>(v_out), vsb, vsh, vsn, stream);
+  if (e != hipSuccess) return hip_fail(e, "kv4_load");
+  return ok();
+}
+
+size_t carnator_kv4_attn_workspace_size(const carnator_kv4 *cache, int32_t heads, int32_t n_rows, int32_t batch,
+                                        int32_t width, int32_t max_q) {
+  if (check_kv4(cache) || check_kv4_attn_sizes(cache, heads, n_rows, batch, width, max_q)) return 0;
+  if (n_rows == 0) return 0;
+  return kv4_attn_scratch_bytes(attn_of(cache, heads, n_rows, batch, width, max_q));
+}
+
+int carnator_kv4_attn(const carnator_rows *q, int32_t n_rows, int32_t heads, const carnator_kv4 *cache,
+                      const int32_t *table, int32_t batch, int32_t width, const int32_t *q_start,
+                      const int32_t *kv_len, int32_t max_q, int32_t causal, float scale, void *out, int64_t ost,
+                      int64_t osh, float *lse, void *workspace, size_t ws_bytes, hipStream_t stream) {
+  int rc;
+  if ((rc = check_kv4(cache))) return rc;
+  if ((rc = check_kv4_attn_sizes(cache, heads, n_rows, batch, width, max_q))) return rc;
+  if ((rc = check_table(table, batch, width, cache->block))) return rc;
+  if (!q_start || !kv_len) return fail(CARNATOR_E_NULL, "q_start and kv_len must be non-NULL");
+  if (!isfinite(scale)) return fail(CARNATOR_E_SHAPE, "scale must be finite");
+  if (n_rows == 0) return ok();
+  if ((rc = check_rows(q, "q"))) return rc;
+  if (!out) return fail(CARNATOR_E_NULL, "out is NULL");
+  if (reinterpret_cast<uintptr_t>(out) % 16 != 0) return fail(CARNATOR_E_ALIGN, "out must be 16-byte aligned");
+  if (ost % 8 || osh % 8) return fail(CARNATOR_E_ALIGN, "out strides must be multiples of 8");
+  if (ost < cache->head_dim || (heads > 1 && osh < cache->head_dim))
+    return fail(CARNATOR_E_SHAPE, "out strides out of range (at least head_dim)");
+  if (misaligned4({table, q_start, kv_len, lse}))
+    return fail(CARNATOR_E_ALIGN, "table, q_start, kv_len and lse must be 4-byte aligned");
+  Kv4Attn a = attn_of(cache, heads, n_rows, batch, width, max_q);
+  if (kv4_attn_workgroups(a) > kMaxWorkgroups)
+    return fail(CARNATOR_E_UNSUPPORTED, "batch * kv_heads * max_q needs %lld workgroups; at most %lld",
+                (long long)kv4_attn_workgroups(a), (long long)kMaxWorkgroups);
+  if ((rc = check_ws(workspace, ws_bytes, kv4_attn_scratch_bytes(a)))) return rc;
+  a.q = to_rows(q);
+  a.table = table;
+  a.q_start = q_start;
+  a.kv_len = kv_len;
+  a.causal = causal != 0;
+  a.c2 = (scale > 0.f ? scale : (float)(1.0 / sqrt((double)cache->head_dim))) * 1.4426950408889634f;
+  a.out = static_cast<uint16_t *>(out);
+  a.ost = ost;
+  a.osh = osh;
+  a.lse = lse;
+  hipError_t e = launch_kv4_attn(a, workspace, stream);
+  if (e != hipSuccess) return hip_fail(e, "kv4_attn");
+  return ok();
 }
 
 // ---------------------------------------------------------------- signature scan

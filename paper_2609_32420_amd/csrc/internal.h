@@ -186,6 +186,54 @@ hipError_t launch_bsattn(View q, View k, View v, uint16_t *out, int64_t osb, int
                          const int32_t *col_idx, const int32_t *order, const int32_t *n_rows,
                          float scale, float *lse, hipStream_t s);
 
+// ---- 4-bit cached keys and values ----------------------------------------------
+// Pages of 64 or 128 tokens (block = 1 << shift), the format of include/carnator.h.
+struct Kv4 {
+  unsigned char *pages;
+  int n_pages, heads, d, shift;
+};
+// Bytes of one head in a page: codes and scales of K, then those of V.
+__host__ __device__ constexpr int kv4_codes(int d, int block) { return block * d / 2; }
+__host__ __device__ constexpr int kv4_scales(int d, int block) { return block * d / 32; }
+__host__ __device__ constexpr int kv4_head_bytes(int d, int block) {
+  return 2 * (kv4_codes(d, block) + kv4_scales(d, block));
+}
+// Strided bf16 [rows, heads, d] tensor in element units.
+struct Rows {
+  const uint16_t *data;
+  int64_t st, sh;
+};
+
+// Requests of one page plan: their starts and first pages sit in LDS.
+constexpr int kMaxPlanBatch = 16384;
+hipError_t launch_page_plan(const int32_t *kv_len, const int32_t *new_len, int batch, int32_t *table,
+                            int width, const int32_t *free_pages, int n_free, int shift, int32_t *q_start,
+                            int32_t *kv_len_out, int32_t *slots, int32_t *positions, int n_slots,
+                            int32_t *counts, hipStream_t s);
+hipError_t launch_kv4_store(Kv4 c, Rows k, Rows v, int n_rows, const int32_t *slots, hipStream_t s);
+hipError_t launch_kv4_load(Kv4 c, const int32_t *table, int batch, int width, const int32_t *kv_len, int n,
+                           uint16_t *ko, int64_t ksb, int64_t ksh, int64_t ksn, uint16_t *vo, int64_t vsb,
+                           int64_t vsh, int64_t vsn, hipStream_t s);
+
+// Attention over the pages: what the kernels read and write.
+struct Kv4Attn {
+  Rows q;
+  int n_rows, heads, group;  // group: query heads to a cached one
+  Kv4 c;
+  const int32_t *table;
+  int batch, width;
+  const int32_t *q_start, *kv_len;
+  int max_q, causal;
+  float c2;  // scale * log2 e
+  uint16_t *out;
+  int64_t ost, osh;
+  float *lse;
+};
+// Largest launch of a call, and its scratch.
+int64_t kv4_attn_workgroups(const Kv4Attn &a);
+size_t kv4_attn_scratch_bytes(const Kv4Attn &a);
+hipError_t launch_kv4_attn(const Kv4Attn &a, void *scratch, hipStream_t s);
+
 // ---- signature scan ----------------------------------------------------------
 // sims: fp64 [nq][m] scratch.
 hipError_t launch_sig(const float *query, int64_t nq, const float *bank, int64_t m, int64_t dim,

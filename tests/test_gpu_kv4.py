@@ -1,0 +1,565 @@
+"""Cached keys and values in 4 bits on the GPU, through the C ABI: bytes of the
+pages, values read back and page plans exactly as the oracle has them, the
+attention against fp64 within bounds that count its roundings."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2609_32420_amd as P
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _bf16(*shape, seed=0, spread=0.0):
+    g = _gen(seed)
+    x = torch.randn(*shape, generator=g, device=DEV)
+    if spread:
+        x = x * torch.exp2(spread * torch.randn(*shape[:-1], 1, generator=g, device=DEV))
+    return x.to(torch.bfloat16)
+
+
+def _f64(x):
+    return x.double().cpu().numpy()
+
+
+# ---------------------------------------------------------------- store and load
+
+def _check_store(pool, k, v, slots, block):
+    want = oracle.kv4_store(pool.cpu().numpy().copy(), _f64(k), _f64(v), slots, block)
+    P.kv4_store(pool, k, v, _i32(slots), block)
+    np.testing.assert_array_equal(pool.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("d,block", [(64, 64), (128, 64), (64, 128), (128, 128)])
+@pytest.mark.parametrize("rows,heads", [(1, 1), (7, 3), (8, 2), (41, 5)])
+def test_store_writes_the_oracles_bytes_and_no_others(d, block, rows, heads):
+    pool = torch.randint(0, 256, (4, heads, block * d * 17 // 16), generator=_gen(rows), device=DEV, dtype=torch.uint8)
+    k, v = _bf16(rows, heads, d, seed=1, spread=6), _bf16(rows, heads, d, seed=2, spread=6)
+    slots = np.random.default_rng(rows).permutation(4 * block)[:rows]
+    slots[rows // 2] = -1
+    if rows > 3:
+        slots[0], slots[3] = 4 * block, -2 ** 31  # out of range
+    _check_store(pool, k, v, slots.tolist(), block)
+
+
+@pytest.mark.parametrize("first,gap", [(0, None), (8, None), (3, None), (60, None), (8, 11), (16, 0)])
+def test_store_of_runs_of_slots(first, gap):
+    # eight rows at a time are one store of V where their slots are an aligned run
+    d, block, rows = 128, 64, 29
+    pool = torch.randint(0, 256, (3, 2, block * d * 17 // 16), generator=_gen(5), device=DEV, dtype=torch.uint8)
+    slots = list(range(first, first + rows))
+    if gap is not None:
+        slots[gap] = -1
+    _check_store(pool, _bf16(rows, 2, d, seed=3), _bf16(rows, 2, d, seed=4), slots, block)
+
+
+def test_store_of_every_bf16_value():
+    # each value beside a larger one of its group or alone in it; infinities and NaN
+    x = torch.arange(65536, device=DEV, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    one = torch.zeros(4096, 1, 64, dtype=torch.bfloat16, device=DEV)
+    one.view(-1, 4, 16)[:, 0, 3] = x[:65536:1].view(-1)[: 4096 * 64 // 64]
+    k = x.view(1024, 1, 64)
+    v = torch.where(torch.arange(64, device=DEV) % 32 == 9, 5 * x.view(1024, 1, 64).roll(1, 0), x.view(1024, 1, 64))
+    pool = torch.zeros(80, 1, 64 * 64 * 17 // 16, dtype=torch.uint8, device=DEV)
+    P.kv4_store(pool, k, v, _i32(list(range(1024))), 64)
+    P.kv4_store(pool, one, one, _i32(list(range(1024, 5120))), 64)
+    kl, vl = P.kv4_load(pool, _i32([list(range(80))]), _i32([5120]), 64)
+    for got, x in ((kl[0, :, :1024], k), (vl[0, :, :1024], v), (kl[0, :, 1024:], one)):
+        want = oracle.kv4_values(*oracle.kv4_quantise(_f64(x)))
+        np.testing.assert_array_equal(_f64(got).transpose(1, 0, 2), want)
+
+
+def test_store_from_a_fused_projection_and_a_broadcast_head():
+    qkv = _bf16(13, 3, 4, 64, seed=7)
+    pool = torch.zeros(2, 4, 64 * 64 * 17 // 16, dtype=torch.uint8, device=DEV)
+    slots = list(range(20, 33))
+    _check_store(pool, qkv[:, 1], qkv[:, 2], slots, 64)
+    _check_store(pool, qkv[:, 1, :1].expand(13, 4, 64), qkv[:, 2].transpose(0, 1).contiguous().transpose(0, 1), slots, 64)
+
+
+def test_store_of_no_rows_and_of_none_in_range():
+    pool = torch.full((1, 1, 64 * 64 * 17 // 16), 7, dtype=torch.uint8, device=DEV)
+    e = torch.empty(0, 1, 64, dtype=torch.bfloat16, device=DEV)
+    P.kv4_store(pool, e, e, _i32([]), 64)
+    P.kv4_store(pool, _bf16(3, 1, 64), _bf16(3, 1, 64), _i32([-1, -1, -1]), 64)
+    assert (pool == 7).all()
+
+
+def _filled(pages, heads, d, block, seed):
+    """A pool whose every token was stored, with unlike scales."""
+    pool = P.kv4_pool(pages, heads, d, block)
+    n = pages * block
+    P.kv4_store(pool, _bf16(n, heads, d, seed=seed, spread=1), _bf16(n, heads, d, seed=seed + 1, spread=1),
+                torch.arange(n, dtype=torch.int32, device=DEV), block)
+    return pool
+
+
+@pytest.mark.parametrize("d,block,heads", [(64, 64, 3), (128, 64, 1), (64, 128, 1), (128, 128, 2)])
+def test_load_reads_the_oracles_values_and_leaves_other_rows(d, block, heads):
+    pool = _filled(6, heads, d, block, 11)
+    host = pool.cpu().numpy()
+    table = [[3, 1, 5], [0, -1, 2], [6, 4, 4], [1, 1, 1]]  # page 6 is none; one page twice
+    kv_len = [3 * block, 2 * block + 37, 4 * block, 0]  # the third is clamped to the table
+    n = 2 * block + 43
+    out = [torch.full((4, n, heads, d), 9.0, dtype=torch.bfloat16, device=DEV).transpose(1, 2) for _ in range(2)]
+    k, v = P.kv4_load(pool, _i32(table), _i32(kv_len), block, out=out)
+    assert k is out[0]
+    for b in range(4):
+        wk, wv, there = oracle.kv4_cached(host, table[b], min(kv_len[b], n), block, d)
+        m = len(there)
+        for got, want in ((k, wk), (v, wv)):
+            np.testing.assert_array_equal(_f64(got[b])[:, :m][:, there], want[:, there])
+            left = torch.ones(n, dtype=torch.bool)
+            left[:m] = torch.tensor(~there)
+            assert (got[b][:, left.to(DEV)] == 9).all()
+    k, v = P.kv4_load(pool, _i32(table), _i32([-5, 1, 0, 1]), block)
+    assert k.shape == (4, heads, 3 * block, d) and (k[0] == 0).all() and (v[2] == 0).all()
+    assert (k[1, :, 1:] == 0).all() and (k[1, :, 0] != 0).any()
+
+
+def test_pages_past_four_gib():
+    # byte offsets of the last pages do not fit 32 bits
+    heads, d, block = 40, 128, 128
+    per = heads * block * d * 17 // 16
+    pages = (1 << 32) // per + 40
+    pool = torch.empty(pages, heads, per // heads, dtype=torch.uint8, device=DEV)
+    table = _i32([[pages - 1, 0, pages - 2]])
+    slots = torch.cat([(pages - 1) * block + torch.arange(block), torch.arange(block),
+                       (pages - 2) * block + torch.arange(60)]).to(torch.int32).to(DEV)
+    k, v = _bf16(316, heads, d, seed=1), _bf16(316, heads, d, seed=2)
+    P.kv4_store(pool, k, v, slots, block)
+    kl, vl = P.kv4_load(pool, table, _i32([316]), block, n=316)
+    rows = [0, 127, 128, 255, 256, 315]
+    for got, x in ((kl, k), (vl, v)):
+        np.testing.assert_array_equal(_f64(got[0, :, rows]).transpose(1, 0, 2),
+                                      oracle.kv4_values(*oracle.kv4_quantise(_f64(x[rows]))))
+    _check_attn(_bf16(70, heads, d, seed=3), pool, table, [0, 70], [316], block, True)
+    _check_attn(_bf16(1, heads, d, seed=3), pool, table, [0, 1], [316], block, True)
+    del pool
+
+
+# ---------------------------------------------------------------- page plan
+
+def _check_plan(kv, new, table, free, block, n_slots):
+    want = oracle.page_plan(kv, new, table, free, block, n_slots)
+    t = _i32(table)
+    for positions in (True, False):
+        t = _i32(table)
+        B = len(kv)
+        out = [torch.full((n,), 77, dtype=torch.int32, device=DEV) for n in (B + 1, B, n_slots, n_slots, 3)]
+        if not positions:
+            out[3] = None
+        got = P.page_plan(_i32(kv), _i32(new), t, _i32(free), block, n_slots, out=out)
+        for g, w, name in zip(got, want, ("q_start", "kv_len", "slots", "positions", "counts")):
+            if g is not None:
+                np.testing.assert_array_equal(g.cpu().numpy(), w, err_msg=name)
+        np.testing.assert_array_equal(t.cpu().numpy(), want[5], err_msg="table")
+
+
+@pytest.mark.parametrize("block", [64, 128])
+@pytest.mark.parametrize("batch,width,most,free,extra", [
+    (1, 1, 1, 1, 0), (1, 4, 200, 9, 3), (5, 3, 150, 100, 0), (64, 40, 1, 64, 0), (64, 40, 1, 5, 6), (33, 6, 300, 40, -500),
+    (257, 2, 90, 300, 5), (1000, 3, 70, 700, 0), (3, 2, 900, 100, 2), (7, 5, 0, 3, 4), (300, 9, 400, 0, 1)])
+def test_plan(block, batch, width, most, free, extra):
+    rng = np.random.default_rng(batch * 7 + most)
+    kv = rng.integers(0, max(1, width * block - most // 2), batch)
+    new = rng.integers(0, most + 1, batch) if most > 1 else np.full(batch, most)
+    new[rng.random(batch) < 0.2] = 0
+    ids = rng.permutation(batch * width + free)
+    table = np.full((batch, width), -1)
+    for b in range(batch):
+        full = -(-int(kv[b]) // block)
+        table[b, :full] = ids[b * width:b * width + full]
+    if batch > 2:
+        table[2, 0] = -1  # a page left out: its tokens have no slot
+    n_slots = max(0, int(new.sum()) + extra)
+    _check_plan(kv.tolist(), new.tolist(), table.tolist(), ids[batch * width:].tolist(), block, n_slots)
+
+
+def test_plan_of_lengths_out_of_range():
+    # lengths below 0 are none, lengths past the table are full
+    _check_plan([-3, 1000, 64], [5, 4, -9], [[-1, -1], [3, 4], [5, -1]], [8, 9], 64, 12)
+    _check_plan([0], [2 ** 31 - 1], [[-1]], [8], 64, 100)
+    _check_plan([0, 3], [2 ** 31 - 1, 2 ** 31 - 1], [[-1], [2]], [8, 9], 64, 70)
+
+
+def test_plan_of_the_largest_batch():
+    rng = np.random.default_rng(1)
+    batch = 16384
+    new = rng.integers(0, 3, batch)
+    kv = rng.integers(0, 120, batch)
+    table = np.where(np.arange(2)[None] < -(-kv // 64)[:, None], np.arange(2 * batch).reshape(batch, 2), -1)
+    _check_plan(kv.tolist(), new.tolist(), table.tolist(), list(range(2 * batch, 2 * batch + 900)), 64, int(new.sum()))
+
+
+# ---------------------------------------------------------------- attention
+
+def _check_attn(q, pool, table, q_start, kv_len, block, causal, scale=0.0, **kw):
+    """Against fp64 over the values that kv4_load reads (exactly, see above).
+
+    With A = sum_j p_j |v_j| over the normalised weights: a score is off by at
+    most `off` (fp32 products of d terms and the factor), so a weight by 2 off
+    relative to their sum; each P is rounded to bf16 (half a step 2^-8) and
+    divided by the sum of the rounded ones, 2^-7 in all; n fp32 additions add
+    n 2^-23; the output is rounded to bf16, 2^-8 |o|.  A weight below the least
+    normal fp32 number may be lost: their sum is at least 1 (that of the
+    reference), so n of them are 2^-126 n max |v| at most."""
+    T, heads, d = q.shape
+    group = heads // pool.shape[1]
+    sigma = scale if scale > 0 else 1 / math.sqrt(d)
+    out = torch.full_like(q, 7.0)
+    lse = torch.full((T, heads), 7.0, device=DEV)
+    o, l = P.kv4_attn(q, pool, table, _i32(q_start), _i32(kv_len), kw.pop("max_q", max(1, max(
+        b - a for a, b in zip(q_start, q_start[1:])))), block, causal=causal, scale=scale, return_lse=True, out=out,
+        lse=lse, **kw)
+    k, v = P.kv4_load(pool, table, _i32(kv_len), block)
+    there = (table >= 0) & (table < pool.shape[0])
+    done = torch.zeros(T, dtype=torch.bool, device=DEV)
+    for b, (a, e) in enumerate(zip(q_start, q_start[1:])):
+        if e <= a:
+            continue
+        done[a:e] = True
+        n = min(max(kv_len[b], 0), table.shape[1] * block)
+        seen = there[b].repeat_interleave(block)[None, :n].expand(e - a, n)
+        if causal:
+            seen = seen & (torch.arange(n, device=DEV)[None] <= n - (e - a) + torch.arange(e - a, device=DEV)[:, None])
+        for h in range(heads):
+            x, kk, vv = q[a:e, h].double(), k[b, h // group, :n].double(), v[b, h // group, :n].double()
+            s = (sigma * (x @ kk.T)).masked_fill(~seen, -math.inf)
+            off = (sigma * (x.abs() @ kk.abs().T)).masked_fill(~seen, 0).amax(1, keepdim=True) if n else 0
+            off = (off * (d + 8) * 2.0 ** -24) if n else torch.zeros(e - a, 1, device=DEV, dtype=torch.float64)
+            ls = torch.logsumexp(s, 1, keepdim=True) if n else torch.full((e - a, 1), -math.inf, device=DEV,
+                                                                            dtype=torch.float64)
+            p = torch.where(seen & torch.isfinite(ls), torch.exp(s - ls), 0.0)
+            want, size = p @ vv, p @ vv.abs()
+            vmax = vv.abs().max().item() if n else 0.0
+            bound = 2.0 ** -8 * want.abs() + (2.0 ** -7 * 1.01 + 2 * off + n * 2.0 ** -23) * size + n * 2.0 ** -126 * vmax
+            got = o[a:e, h].double()
+            assert ((got - want).abs() <= bound).all(), (b, h, ((got - want).abs() / bound).max().item())
+            gl = l[a:e, h].double()[:, None]
+            some = torch.isfinite(ls)
+            assert torch.equal(some, torch.isfinite(gl)) and (gl[~some] == -math.inf).all()
+            assert ((gl - ls).abs()[some] <= (off + n * 2.0 ** -23 + 2.0 ** -22 + ls.abs() * 2.0 ** -23)[some]).all()
+    assert (o[~done] == 7).all() and (l[~done] == 7).all()
+    # the same bits again, without the LSE, and in an output of the call's own
+    again = P.kv4_attn(q, pool, table, _i32(q_start), _i32(kv_len), max(1, max(b - a for a, b in zip(q_start, q_start[1:]))),
+                       block, causal=causal, scale=scale)
+    assert torch.equal(again[done].view(torch.int16), o[done].view(torch.int16)) and (again[~done] == 0).all()
+    return o, l
+
+
+def _tables(kv_len, block, pages, seed, width=None):
+    rng = np.random.default_rng(seed)
+    ids = rng.permutation(pages)
+    width = width or max(1, max(-(-n // block) for n in kv_len))
+    t, at = np.full((len(kv_len), width), -1), 0
+    for b, n in enumerate(kv_len):
+        m = min(width, -(-n // block))
+        t[b, :m] = ids[at:at + m]
+        at += m
+    return _i32(t.tolist())
+
+
+LENGTHS = [([1], [1]), ([1], [31]), ([1], [64]), ([1, 1, 1], [33, 129, 2]), ([2, 1, 0, 5], [500, 1, 77, 5]),
+           ([1, 1], [1500, 40]), ([17, 3, 1], [17, 290, 1000]), ([70, 1], [333, 700]), ([130, 20, 257], [130, 300, 600]),
+           ([1, 300], [2100, 1300])]
+
+
+@pytest.mark.parametrize("d,block", [(64, 64), (128, 64), (64, 128), (128, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("case", range(len(LENGTHS)))
+def test_attention(d, block, causal, case):
+    m, kv = LENGTHS[case]
+    kv_heads, group = [(2, 1), (1, 4), (3, 7), (2, 8)][(case + d // 64 + block // 64) % 4]
+    pages = sum(-(-n // block) for n in kv) + 2
+    pool = _filled(pages, kv_heads, d, block, case)
+    start = [1] + (1 + np.cumsum(m)).tolist()
+    q = _bf16(start[-1] + 2, kv_heads * group, d, seed=case + 50)
+    _check_attn(q, pool, _tables(kv, block, pages, case), start, kv, block, causal)
+
+
+@pytest.mark.parametrize("group", [1, 2, 3, 5, 16, 20, 40, 71])
+@pytest.mark.parametrize("m", [1, 4, 9])
+def test_attention_of_many_query_heads(group, m):
+    pool = _filled(8, 1, 64, 64, 3)
+    kv = [300, 90]
+    _check_attn(_bf16(2 * m, group, 64, seed=group), pool, _tables(kv, 64, 8, 1), [0, m, 2 * m], kv, 64, True)
+
+
+@pytest.mark.parametrize("m", [1, 3, 90, 200])
+def test_attention_rows_that_see_nothing(m):
+    # fewer tokens than causal queries, no tokens, every page left out, no queries
+    pool = _filled(6, 2, 128, 64, 9)
+    table = _i32([[0, 1, -1], [-1, -1, -1], [-1, -1, 6], [2, -1, 3], [4, 5, -1]])
+    kv = [max(1, m - 2), 0, 192, 150, 100]
+    start = [0, m, 2 * m, 3 * m, 4 * m, 4 * m]
+    for causal in (False, True):
+        _check_attn(_bf16(4 * m + 1, 4, 128, seed=m), pool, table, start, kv, 64, causal)
+
+
+def test_attention_of_a_clamped_length_and_strided_queries():
+    pool = _filled(6, 2, 64, 64, 9)
+    table = _tables([192, 192], 64, 6, 2)
+    qkv = _bf16(6, 3, 4, 64, seed=5)
+    out = torch.zeros(6, 4, 64, dtype=torch.bfloat16, device=DEV)
+    a = P.kv4_attn(qkv[:, 0].contiguous(), pool, table, _i32([0, 3, 6]), _i32([192, 192]), 3, 64, causal=True)
+    big = torch.full((6, 8, 64), 3.0, dtype=torch.bfloat16, device=DEV)
+    P.kv4_attn(qkv[:, 0], pool, table, _i32([0, 3, 6]), _i32([100000, 192]), 50, 64, causal=True, out=big[:, 2:6])
+    assert torch.equal(big[:, 2:6], a) and (big[:, :2] == 3).all() and (big[:, 6:] == 3).all()
+    # heads before tokens, as [1, H, N, d] storage has them
+    qt = qkv[:, 0].transpose(0, 1).contiguous().transpose(0, 1)
+    ot = out.transpose(0, 1).contiguous().transpose(0, 1)
+    P.kv4_attn(qt, pool, table, _i32([0, 3, 6]), _i32([192, 192]), 3, 64, causal=True, out=ot)
+    assert torch.equal(ot, a)
+
+
+@pytest.mark.parametrize("m", [1, 40, 150])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_large_and_shifted_scores(m, d):
+    # scores of a few hundred, climbing or falling along the keys, all far below 0
+    block, n, heads = 64, 700, 2
+    ramp = torch.linspace(0, 1, n, device=DEV)[:, None, None]
+    for seed, (a, b) in enumerate([(30.0, 0.0), (0.0, 40.0), (40.0, -40.0), (-60.0, 0.0)]):
+        k = (_bf16(n, heads, d, seed=seed).float() + a + b * ramp).to(torch.bfloat16)
+        pool = P.kv4_pool(11, heads, d, block)
+        P.kv4_store(pool, k, _bf16(n, heads, d, seed=9), torch.arange(n, dtype=torch.int32, device=DEV), block)
+        q = (_bf16(m, heads, d, seed=seed + 20).float() + 0.4).to(torch.bfloat16)
+        _check_attn(q, pool, _i32([list(range(11))]), [0, m], [n], block, True)
+        _check_attn(q, pool, _i32([list(range(11))]), [0, m], [n], block, False, scale=1.3)
+
+
+@pytest.mark.parametrize("m", [1, 30, 100, 260])
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_that_are_masked_have_no_effect(m, d):
+    # NaN behind the last token, in a page left out, and in tokens that a causal
+    # query does not see; queries that see one get NaN in its channels alone
+    block, n, heads = 64, 300, 2
+    k, v = _bf16(n, heads, d, seed=1), _bf16(n, heads, d, seed=2)
+    table = _i32([[4, 0, 6, 1, 3]])
+    slots = torch.cat([p * block + torch.arange(64) for p in (4, 0, 6, 1, 3)])[:n].to(torch.int32).to(DEV)
+    clean = P.kv4_pool(7, heads, d, block)
+    P.kv4_store(clean, k, v, slots, block)
+    pool = torch.full_like(clean, 255)
+    P.kv4_store(pool, k, v, slots, block)
+    hole = table.clone()
+    hole[0, 1] = -1
+    pool[0], args = 255, (_i32([0, m]), _i32([n]), m, block)
+    q = _bf16(m, heads, d, seed=3)
+    for causal in (False, True):
+        a = P.kv4_attn(q, clean, hole, *args, causal=causal, return_lse=True)
+        b = P.kv4_attn(q, pool, hole, *args, causal=causal, return_lse=True)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and torch.isfinite(b[0].float()).all()
+    # V of tokens n - 3 and n - 29, one group of 32 channels each
+    bad_v = v.clone()
+    bad_v[n - 3, 1, 32] = math.nan
+    bad_v[n - 29, 1, 5] = math.inf
+    clean = P.kv4_pool(7, heads, d, block)
+    P.kv4_store(clean, k, v, slots, block)
+    pool = clean.clone()
+    P.kv4_store(pool, k, bad_v, slots, block)
+    a = P.kv4_attn(q, clean, table, *args, causal=True)
+    b = P.kv4_attn(q, pool, table, *args, causal=True)
+    last = n - m + torch.arange(m, device=DEV)  # last token that a query sees
+    nan = torch.zeros(m, heads, d, dtype=torch.bool, device=DEV)
+    nan[last >= n - 3, 1, 32:64] = True
+    nan[last >= n - 29, 1, :32] = True
+    assert torch.equal(torch.isnan(b), nan) and torch.equal(b[~nan], a[~nan])
+    assert torch.equal(torch.isnan(P.kv4_attn(q, pool, table, *args)).any(0).any(0)[:d],
+                       nan[-1].any(0) | torch.zeros(d, dtype=torch.bool, device=DEV))
+    # K of token n - 3: queries that see it have no other answer than NaN
+    bad_k = k.clone()
+    bad_k[n - 3, 0, 7] = -math.inf
+    P.kv4_store(pool, bad_k, v, slots, block)
+    b, lse = P.kv4_attn(q, pool, table, *args, causal=True, return_lse=True)
+    sees = last >= n - 3
+    assert torch.isnan(b[sees, 0]).all() and torch.isnan(lse[sees, 0]).all()
+    assert torch.equal(b[~sees], a[~sees]) and torch.equal(b[sees, 1], a[sees, 1])
+
+
+@pytest.mark.parametrize("m", [1, 200])
+def test_attention_of_a_long_cache(m):
+    # parts of the key axis joined; a request of every length beside it
+    kv = [20011, 64, 1, 4100]
+    pages = sum(-(-n // 128) for n in kv)
+    pool = _filled(pages, 2, 128, 128, 4)
+    _check_attn(_bf16(4 * m, 4, 128, seed=m), pool, _tables(kv, 128, pages, 3), [m * i for i in range(5)], kv, 128, True)
+
+
+def test_a_workspace_is_used_up_to_its_size():
+    pool = _filled(60, 2, 64, 64, 4)
+    table, q = _tables([3800], 64, 60, 3), _bf16(2, 8, 64, seed=1)
+    args = (_i32([0, 2]), _i32([3800]), 2, 64)
+    want = P.kv4_attn(q, pool, table, *args, causal=True)
+    size = P.kv4_attn_workspace(q, pool, table, 2, 64).numel()
+    buf = torch.full((size + 512,), 0xAB, dtype=torch.uint8, device=DEV)
+    assert torch.equal(P.kv4_attn(q, pool, table, *args, causal=True, workspace=buf[:size]), want)
+    assert (buf[size:] == 0xAB).all()
+
+
+def test_another_stream_and_a_captured_graph():
+    block, heads, d = 64, 2, 128
+    cache = P.Kv4Cache(40, 2, 20, heads, d, block)
+    cache.append(_bf16(700, heads, d, seed=1), _bf16(700, heads, d, seed=2), _i32([500, 200]))
+    kv, table, free = cache.kv_len.clone(), cache.table.clone(), cache.free.clone()
+    k, v, q = _bf16(2, heads, d, seed=3), _bf16(2, heads, d, seed=4), _bf16(2, 4, d, seed=5)
+    ones, wide = _i32([1, 1]), _bf16(180, 4, d, seed=6)
+
+    def step(pool, table):
+        start, kv_out, slots, pos, counts = P.page_plan(kv, ones, table, free, block, 2)
+        P.kv4_store(pool, k, v, slots, block)
+        o = P.kv4_attn(q, pool, table, start, kv_out, 1, block, causal=True)
+        w = P.kv4_attn(wide, pool, table, _i90, kv_out, 90, block, causal=True)
+        return [o, w, kv_out, slots, *P.kv4_load(pool, table, kv_out, block)]
+
+    _i90 = _i32([0, 90, 180])
+    want = step(cache.pool.clone(), table.clone())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step(cache.pool.clone(), table.clone())
+        pool, t = cache.pool.clone(), table.clone()
+    side.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        held = step(pool, t)
+    for i in range(4):
+        q.copy_(_bf16(2, 4, d, seed=30 + i))
+        k.copy_(_bf16(2, heads, d, seed=40 + i))
+        want = step(cache.pool.clone(), table.clone())  # eager work between the replays
+        t.copy_(table)
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------- together
+
+def test_a_cache_grows_token_by_token():
+    # prompts, single tokens, requests that come and go; against the oracle on
+    # the host's copy of what was stored
+    block, kv_heads, heads, d, batch = 64, 2, 6, 64, 4
+    cache = P.Kv4Cache(16, batch, 5, kv_heads, d, block)
+    ks = [np.zeros((0, kv_heads, d)) for _ in range(batch)]
+    vs = [np.zeros((0, kv_heads, d)) for _ in range(batch)]
+    steps = [[60, 130, 1, 0], [1, 1, 1, 1], [5, 0, 3, 64], [1, 1, 1, 1]]
+    for step, new in enumerate(steps):
+        rows = sum(new)
+        k, v = _bf16(rows + 1, kv_heads, d, seed=step), _bf16(rows + 1, kv_heads, d, seed=step + 9)
+        q = _bf16(rows + 1, heads, d, seed=step + 30)
+        held = [x.shape[0] for x in ks]
+        q_start, positions, lacking = cache.append(k, v, _i32(new))
+        assert lacking == 0 and q_start.tolist() == [0] + np.cumsum(new).tolist()
+        assert positions.tolist() == [held[b] + i for b in range(batch) for i in range(new[b])] + [-1]
+        at = 0
+        for b in range(batch):
+            for x, y in ((ks, k), (vs, v)):
+                x[b] = np.concatenate([x[b], oracle.kv4_values(*oracle.kv4_quantise(_f64(y[at:at + new[b]])))])
+            at += new[b]
+        o = _f64(cache.attn(q, q_start, max(new), causal=True))
+        kl, vl = cache.load()
+        at = 0
+        for b in range(batch):
+            n = ks[b].shape[0]
+            np.testing.assert_array_equal(_f64(kl[b, :, :n]).transpose(1, 0, 2), ks[b])
+            np.testing.assert_array_equal(_f64(vl[b, :, :n]).transpose(1, 0, 2), vs[b])
+            for i in range(new[b]):
+                lim = n - new[b] + i + 1
+                for h in range(heads):
+                    s = ks[b][:lim, h // 3] @ _f64(q[at + i, h]) / 8
+                    p = np.exp(s - s.max())
+                    p /= p.sum()
+                    want, size = p @ vs[b][:lim, h // 3], p @ np.abs(vs[b][:lim, h // 3])
+                    assert (np.abs(o[at + i, h] - want) <= 2 ** -8 * np.abs(want) + 2 ** -6.9 * size).all()
+            at += new[b]
+        assert (o[at:] == 0).all()
+        used = cache.table[cache.table >= 0].tolist()
+        assert len(set(used)) == len(used) and sorted(used + cache.free.tolist()) == list(range(16))
+        if step == 1:
+            cache.release([1])
+            ks[1] = vs[1] = np.zeros((0, kv_heads, d))
+    # a page that two requests share is not freed with the first
+    cache.table[3, 4] = cache.table[0, 0]
+    keep = int(cache.table[0, 0])
+    cache.release([0])
+    assert keep not in cache.free.tolist()
+    # more tokens than there are pages
+    free = cache.free.numel()
+    _, _, lacking = cache.append(_bf16(320, kv_heads, d), _bf16(320, kv_heads, d), _i32([320, 0, 0, 0]))
+    assert lacking == max(0, 320 - 64 * free) and int(cache.kv_len[0]) == min(320, 64 * free)
+
+
+def test_context_of_a_region_from_the_cache():
+    """A middle layer of a cache-hit request: keys and values of the context
+    come from the history's cache, those of the active blocks are the target's
+    own; the block-sparse attention of the active rows reads both."""
+    heads, d, block, N = 2, 64, 64, 64 * 6 - 20
+    grid = (1, 4, 13, 7)
+    hist_k, hist_v = _bf16(N, heads, d, seed=1), _bf16(N, heads, d, seed=2)
+    cache = P.Kv4Cache(8, 1, 6, heads, d, block)
+    assert cache.append(hist_k, hist_v, _i32([N]))[2] == 0
+    evidence = torch.zeros(grid, dtype=torch.uint8, device=DEV)
+    evidence[0, 1, 3, 3] = 1  # active tokens in block 1, context in blocks 1 and 2
+    region, _ = P.region_weights(evidence, 1, 1)
+    active, context = P.region_block_flags(region, 0, block)
+    q, k, v = (_bf16(1, heads, N, d, seed=s) for s in (3, 4, 5))
+    only = context * (1 - active)
+    assert only.any() and active.any()
+    before = k.clone(), v.clone()
+    cache.load(out=(k, v), keep=only)
+    rows = only[0].repeat_interleave(block)[:N].bool()
+    want = oracle.kv4_values(*oracle.kv4_quantise(_f64(hist_k)))
+    np.testing.assert_array_equal(_f64(k[0][:, rows]), want.transpose(1, 0, 2)[:, rows.cpu().numpy()])
+    assert torch.equal(k[:, :, ~rows], before[0][:, :, ~rows]) and torch.equal(v[:, :, ~rows], before[1][:, :, ~rows])
+    bits = P.pack_block_mask(torch.ones(1, heads, 6, 6, dtype=torch.uint8, device=DEV))
+    row_ptr, col_idx, order, n_active = P.compact_block_mask_bits_region(bits, active, context)
+    out = torch.full_like(q, 5.0)
+    P.block_sparse_attn_lists(q, k, v, (row_ptr, col_idx, order), block, out=out, n_rows=n_active)
+    mask = np.zeros((1, heads, 6, 6), np.uint8)
+    mask[:] = active[0].cpu().numpy()[:, None] & context[0].cpu().numpy()[None]
+    ro, _ = oracle.block_sparse_attention(_f64(q), _f64(k), _f64(v), mask, block)
+    act = active[0].repeat_interleave(block)[:N].bool()
+    assert (out[:, :, ~act] == 5).all()
+    np.testing.assert_allclose(_f64(out[:, :, act]), ro[:, :, act.cpu().numpy()], atol=2e-2)
+    # the same queries straight over the cached context
+    qa = q[0, :, act].transpose(0, 1)
+    got = cache.attn(qa, _i32([0, qa.shape[0]]), qa.shape[0], keep=only)
+    _check_attn(qa, cache.pool, cache.table.masked_fill(only == 0, -1), [0, qa.shape[0]], [N], block, False)
+    assert got.shape == qa.shape
+
+
+def test_binding_refuses_what_does_not_fit():
+    pool = P.kv4_pool(3, 2, 64, 64)
+    t, one = _i32([[0, 1]]), _i32([5])
+    x = _bf16(4, 2, 64)
+    for f in (lambda: P.kv4_store(pool, x[:, :1], x, _i32([0] * 4), 64), lambda: P.kv4_store(pool, x, x, _i32([0] * 3), 64),
+              lambda: P.kv4_store(pool, x.float(), x, _i32([0] * 4), 64), lambda: P.kv4_store(pool, x, x[:3], _i32([0] * 4), 64),
+              lambda: P.kv4_store(pool[:, :1], x, x, _i32([0] * 4), 64), lambda: P.kv4_store(pool, x, x, one.long(), 64),
+              lambda: P.kv4_load(pool, t, _i32([5, 6]), 64), lambda: P.kv4_load(pool, t.cpu(), one, 64),
+              lambda: P.kv4_load(pool, t, one, 64, out=(x, x)),
+              lambda: P.kv4_attn(x, pool, t, _i32([0, 4, 4]), one, 4, 64),
+              lambda: P.kv4_attn(x[0], pool, t, _i32([0, 4]), one, 4, 64),
+              lambda: P.kv4_attn(x, pool, t, _i32([0, 4]), one, 4, 64, out=x[:2].clone()),
+              lambda: P.kv4_attn(x, pool, t, _i32([0, 4]), one, 4, 64, return_lse=True, lse=torch.zeros(4, 2, device=DEV)[:, :1]),
+              lambda: P.page_plan(one, _i32([1, 1]), t, one, 64, 3)):
+        with pytest.raises(ValueError):
+            f()
+    with pytest.raises(P.CarnatorError):
+        P.kv4_attn(_bf16(4, 3, 64), pool, t, _i32([0, 4]), one, 4, 64)
+    with pytest.raises(P.CarnatorError):
+        P.kv4_store(pool, torch.empty(4 * 128 + 4, dtype=torch.bfloat16, device=DEV)[4:].view(4, 2, 64), x, _i32([0] * 4), 64)

@@ -28,6 +28,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;
 constexpr int kStep = 32;  // tokens of a wave's step
+constexpr int kAhead = 1;  // steps whose loads are under way
+constexpr int kMaxChunks = 256;
 // Growth of the running maximum (log2 units) below which O and l keep their
 // scale: P may then reach 2^8, harmless in fp32 and bf16.
 constexpr float kSlack = 8.f;
@@ -45,6 +47,16 @@ __device__ inline bf16x8 eight_of(uint32_t codes, uint32_t scale) {
                                           pair_of<2>(codes, scale), pair_of<3>(codes, scale)});
 }
 
+// 1 / l; 0 where nothing was seen.
+__device__ inline float inverse(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN; }
+// Natural log-sum-exp from a reference m (log2 units) and the sum beside it:
+// reference, exponent and log2 of the mantissa are added in fp64, since the
+// first two can be large where the result is small.
+__device__ inline float lse_of(float m, float l) {
+  const double l2 = (double)m + (double)__builtin_amdgcn_frexp_expf(l) + (double)__log2f(__builtin_amdgcn_frexp_mantf(l));
+  return l > 0.f ? (float)(l2 * 0.69314718055994531) : l == 0.f ? -INFINITY : NAN;
+}
+
 // What a request's queries are and see.
 struct Span {
   int q0;     // first query row
@@ -56,29 +68,65 @@ struct Span {
   }
 };
 __device__ inline Span span_of(const Kv4Attn &a, int b) {
+  const int q0 = __builtin_amdgcn_readfirstlane(a.q_start[b]), q1 = __builtin_amdgcn_readfirstlane(a.q_start[b + 1]);
+  const int kv = __builtin_amdgcn_readfirstlane(a.kv_len[b]);
   Span s;
-  s.q0 = min(max(a.q_start[b], 0), a.n_rows);
-  s.m = min(max(a.q_start[b + 1], s.q0), a.n_rows) - s.q0;
+  s.q0 = min(max(q0, 0), a.n_rows);
+  s.m = min(max(q1, s.q0), a.n_rows) - s.q0;
   s.rows = min(s.m, a.max_q) * a.group;
-  s.kv = min(max(a.kv_len[b], 0), a.width << a.c.shift);
+  s.kv = min(max(kv, 0), a.width << a.c.shift);
   return s;
 }
+// Tokens that the last of 16 NT rows from row0 on sees: what a tile walks.
+__device__ inline int tile_end(const Kv4Attn &a, const Span &s, int row0, int rows) {
+  return s.limit(a, (min(row0 + rows, s.rows) - 1) / a.group);
+}
 
-template <int D, int NT>
-__global__ void __launch_bounds__(64 * kWaves, 2)
-rows_kernel(Kv4Attn a, int tiles) {
+// How a call is cut: row tiles, and parts of the key axis of `chunk` tokens
+// whose results a second kernel joins.
+struct Cut {
+  int tiles, chunk, chunks;
+};
+// Results of the parts: outputs [n_rows * heads][chunks][d] not yet divided,
+// (reference, rounded sum, sum) beside them.
+struct Parts {
+  float *o;
+  float4 *ml;
+};
+
+// What a wave reads of 32 tokens.
+template <int D>
+struct Raw {
+  u32x4 k[2];        // 16 (8 at d = 64) bytes of a token
+  uint32_t ks[2];    // their scale
+  u32x4 v[D / 64];   // two channel pairs of an octet
+  uint2 vs[D / 64];  // the octet's scales
+};
+
+template <int D, int NT, bool SPLIT>
+__global__ void __launch_bounds__(64 * kWaves, NT == 1 ? 3 : 2)
+rows_kernel(Kv4Attn a, Cut cut, Parts parts) {
   constexpr int TQ = D / 32;        // products of a key tile
   constexpr int CPL = D / 4;        // channels of a lane
   constexpr int NV = D / 64;        // 64-channel parts of V
-  extern __shared__ float lds_o[];  // [2][NT * NV * 16][64] outputs, then [2][NT][2][64] maxima and sums
+  extern __shared__ float lds_o[];  // [2][NT * NV * 16][64] outputs, then [2][NT][3][64] references and sums
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, j = lane >> 4;
-  const int tile = (int)blockIdx.x % tiles;
-  const int bh = (int)blockIdx.x / tiles;
-  const int b = bh / a.c.heads, h = bh - b * a.c.heads;
+  int id = (int)blockIdx.x;
+  const int h = id % a.c.heads;
+  id /= a.c.heads;
+  const int tile = id % cut.tiles;
+  id /= cut.tiles;
+  const int b = id % a.batch, chunk = SPLIT ? id / a.batch : 0;
   const Span sp = span_of(a, b);
   const int row0 = tile * 16 * NT;
   if (row0 >= sp.rows) return;
+  const int end = tile_end(a, sp, row0, 16 * NT);  // tokens that a row of the tile sees
+  const int k_first = SPLIT ? chunk * cut.chunk : 0;
+  if (k_first >= end && chunk > 0) return;
+  const bool whole = !SPLIT || end <= cut.chunk;  // nothing to join
+  const int k_end = SPLIT ? min(end, k_first + cut.chunk) : end;
+  const int seen_by_all = sp.limit(a, row0 / a.group);
 
   // ---- Q: query column r of each 16, channels CPL j + 8 t .. + 8
   bf16x8 qf[NT][TQ];
@@ -97,9 +145,6 @@ rows_kernel(Kv4Attn a, int tiles) {
       qf[n][t] = __builtin_bit_cast(bf16x8, w);
     }
   }
-  // tokens that every row of the tile sees, and that one of them sees
-  const int seen_by_all = sp.limit(a, row0 / a.group);
-  const int end = sp.limit(a, (min(row0 + 16 * NT, sp.rows) - 1) / a.group);
 
   f32x4 o[NT][NV][4];
   float mrun[NT], lrun[NT], lexact[NT];
@@ -117,58 +162,92 @@ rows_kernel(Kv4Attn a, int tiles) {
   const int rec = kv4_head_bytes(D, block);
   const int codes = kv4_codes(D, block), scales = kv4_scales(D, block);
   const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
-  for (int k0 = wave * kStep; k0 < end; k0 += kWaves * kStep) {
-    const int page = __builtin_amdgcn_readfirstlane(a.table[(int64_t)b * a.width + (k0 >> a.c.shift)]);
-    if ((unsigned)page >= (unsigned)a.c.n_pages) continue;
+
+  // ---- the wave's steps: pages come from the table 64 entries at a time
+  int entry0 = k_first >> a.c.shift;  // of lane 0
+  int entry = -1;
+  auto look = [&]() {
+    entry = -1;
+    if (entry0 + lane < a.width) entry = a.table[(int64_t)b * a.width + entry0 + lane];
+  };
+  look();
+  int page = -1;
+  // the first of the wave's steps from k0 on that has a page
+  auto next = [&](int k0) {
+    for (; k0 < k_end; k0 += kWaves * kStep) {
+      int at = (k0 >> a.c.shift) - entry0;
+      if (at >= 64) {
+        entry0 += at;
+        at = 0;
+        look();
+      }
+      page = __builtin_amdgcn_readlane(entry, at);
+      if ((unsigned)page < (unsigned)a.c.n_pages) break;
+    }
+    return k0;
+  };
+  // K: tile T, MFMA row r is token 8 (r >> 2) + 4 T + (r & 3); V: octet j,
+  // channels 64 v + 4 r .. + 4
+  // (unsigned offsets from a scalar address: no 64-bit vector additions)
+  const unsigned k_tok = 8 * (r >> 2) + (r & 3);
+  const unsigned k_off = k_tok * (D / 2) + CPL / 2 * j, ks_off = k_tok * (D / 32) + j * CPL / 32;
+  const unsigned v_off = (j * (D / 2) + 2 * r) * 8, vs_off = (j * (D / 32) + (r >> 3)) * 8;
+  auto load = [&](Raw<D> &x, int k0) {
     const unsigned char *base = a.c.pages + ((int64_t)page * a.c.heads + h) * rec;
     const int tp = k0 & (block - 1);
-    // ---- K: tile T, MFMA row r is token 8 (r >> 2) + 4 T + (r & 3)
-    bf16x8 kf[2][TQ];
+    const unsigned char *kb = base + tp * (D / 2), *ks = base + codes + tp * (D / 32);
+    const unsigned char *vb = base + codes + scales + tp * (D / 2), *vs = base + 2 * codes + scales + tp * (D / 32);
 #pragma unroll
     for (int T = 0; T < 2; ++T) {
-      const int tok = tp + 8 * (r >> 2) + 4 * T + (r & 3);
-      const uint32_t sc = (uint32_t)base[codes + tok * (D / 32) + j * CPL / 32] << 23;
       if constexpr (D == 128) {
-        const u32x4 w = *reinterpret_cast<const u32x4 *>(base + tok * (D / 2) + 16 * j);
-#pragma unroll
-        for (int t = 0; t < TQ; ++t) kf[T][t] = eight_of(w[t], sc);
+        x.k[T] = *reinterpret_cast<const u32x4 *>(kb + (k_off + 4 * T * (D / 2)));
       } else {
-        const uint2 w = *reinterpret_cast<const uint2 *>(base + tok * (D / 2) + 8 * j);
-        kf[T][0] = eight_of(w.x, sc);
-        kf[T][1] = eight_of(w.y, sc);
+        const uint2 w = *reinterpret_cast<const uint2 *>(kb + (k_off + 4 * T * (D / 2)));
+        x.k[T] = u32x4{w.x, w.y, 0, 0};
       }
+      x.ks[T] = ks[ks_off + 4 * T * (D / 32)];
     }
-    // ---- V: octet j; channels 64 v + 4 r .. + 4 (two pairs)
-    u32x4 vw[NV];
-    uint2 vs[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const unsigned char *vb = base + codes + scales;
-      vw[v] = *reinterpret_cast<const u32x4 *>(vb + (((tp >> 3) + j) * (D / 2) + 32 * v + 2 * r) * 8);
-      vs[v] = *reinterpret_cast<const uint2 *>(vb + codes + (((tp >> 3) + j) * (D / 32) + 2 * v + (r >> 3)) * 8);
+      x.v[v] = *reinterpret_cast<const u32x4 *>(vb + (v_off + 256 * v));
+      x.vs[v] = *reinterpret_cast<const uint2 *>(vs + (vs_off + 16 * v));
     }
+  };
+  auto step = [&](const Raw<D> &x, int k0) {
+    bf16x8 kf[2][TQ];
+#pragma unroll
+    for (int T = 0; T < 2; ++T)
+#pragma unroll
+      for (int t = 0; t < TQ; ++t) kf[T][t] = eight_of(x.k[T][t], x.ks[T] << 23);
+    uint2 vs[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) vs[v] = x.vs[v];
     const bool part = k0 + kStep > seen_by_all;  // a row does not see all of the tokens
-    uint32_t poison[NV][2] = {};  // tokens whose V is NaN, of the two groups of a part
+    uint32_t poison[NV] = {};  // tokens whose V is NaN in this lane's output channels
     if (part) {
       // A token out of a row's sight has P = 0 there, which NaN (or what lies
       // behind the last token) would still turn into NaN: its scale becomes that
       // of byte 0.  Rows that see it get their NaN afterwards.
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
+      for (int v = 0; v < NV; ++v) {
+        uint32_t nan = 0;  // of this lane's octet and group of 32 channels
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           uint32_t &w = e < 4 ? vs[v].x : vs[v].y;
           const uint32_t byte = 0xFFu << (8 * (e & 3));
-          const bool nan = (w & byte) == byte;
-          const bool in = k0 + 8 * j + e < sp.kv;
-          const uint64_t bad = __ballot(nan && in);
-          if (nan || !in) w &= ~byte;
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            poison[v][0] |= (bad >> (16 * g) & 0xFF) ? 1u << (8 * g + e) : 0u;
-            poison[v][1] |= (bad >> (16 * g + 8) & 0xFF) ? 1u << (8 * g + e) : 0u;
-          }
+          const bool in = k0 + 8 * j + e < sp.kv, is_nan = (w & byte) == byte;
+          if (is_nan && in) nan |= 1u << e;
+          if (is_nan || !in) w &= ~byte;
         }
+        // outputs 64 v + 16 j + ..: group 2 v + (j >> 1), read by lanes 8 (j >> 1) .. + 8 of each octet
+        uint32_t p0 = 0, p1 = 0;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          p0 |= (uint32_t)__builtin_amdgcn_readlane((int)nan, 16 * g) << (8 * g);
+          p1 |= (uint32_t)__builtin_amdgcn_readlane((int)nan, 16 * g + 8) << (8 * g);
+        }
+        poison[v] = j < 2 ? p0 : p1;
+      }
     }
     // ---- scores, softmax
     u32x4 p[NT];
@@ -223,11 +302,11 @@ rows_kernel(Kv4Attn a, int tiles) {
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int pr = 0; pr < 2; ++pr) {
-        const uint32_t w0 = vw[v][2 * pr], w1 = vw[v][2 * pr + 1];  // tokens 0-3, 4-7 of a channel pair
-        const uint32_t x = vs[v].x, y = vs[v].y;
-        const uint32_t t0 = pair_of<0>(w0, x << 23), t1 = pair_of<1>(w0, x << 15), t2 = pair_of<2>(w0, x << 7),
-                       t3 = pair_of<3>(w0, x >> 1), t4 = pair_of<0>(w1, y << 23), t5 = pair_of<1>(w1, y << 15),
-                       t6 = pair_of<2>(w1, y << 7), t7 = pair_of<3>(w1, y >> 1);
+        const uint32_t w0 = x.v[v][2 * pr], w1 = x.v[v][2 * pr + 1];  // tokens 0-3, 4-7 of a channel pair
+        const uint32_t lo = vs[v].x, hi = vs[v].y;
+        const uint32_t t0 = pair_of<0>(w0, lo << 23), t1 = pair_of<1>(w0, lo << 15), t2 = pair_of<2>(w0, lo << 7),
+                       t3 = pair_of<3>(w0, lo >> 1), t4 = pair_of<0>(w1, hi << 23), t5 = pair_of<1>(w1, hi << 15),
+                       t6 = pair_of<2>(w1, hi << 7), t7 = pair_of<3>(w1, hi >> 1);
 #pragma unroll
         for (int ch = 0; ch < 2; ++ch) {
           const uint32_t sel = ch ? 0x07060302u : 0x05040100u;
@@ -242,16 +321,36 @@ rows_kernel(Kv4Attn a, int tiles) {
     if (part) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const uint32_t mine = j < 2 ? poison[v][0] : poison[v][1];  // of this lane's output channels
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const int see = limit[n] - k0;
           const uint32_t vis = see >= 32 ? ~0u : see <= 0 ? 0u : (1u << see) - 1;
-          if (mine & vis)
+          if (poison[v] & vis)
 #pragma unroll
             for (int q = 0; q < 4; ++q) o[n][v][q] = f32x4{NAN, NAN, NAN, NAN};
         }
       }
+    }
+  };
+  // the loads of kAhead steps are under way during a step
+  constexpr int NB = kAhead + 1;
+  Raw<D> buf[NB];
+  int at[NB], last = k_first + (wave - kWaves) * kStep;
+  auto fetch = [&](int slot) {
+    at[slot] = last = next(last + kWaves * kStep);
+    if (last < k_end) load(buf[slot], last);
+  };
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s) fetch(s);
+  for (bool more = true; more;) {
+#pragma unroll
+    for (int s = 0; s < NB; ++s) {
+      if (at[s] >= k_end) {
+        more = false;
+        break;
+      }
+      fetch((s + kAhead) % NB);
+      step(buf[s], at[s]);
     }
   }
   // ---- sums over the lanes of a query, then the waves' parts in a fixed order
@@ -312,7 +411,18 @@ rows_kernel(Kv4Attn a, int tiles) {
     const int row = row0 + 16 * n + r;
     if (row >= sp.rows) continue;
     const int i = row / a.group, hd = h * a.group + row - i * a.group;
-    const float inv = lrun[n] > 0.f ? 1.f / lrun[n] : lrun[n] == 0.f ? 0.f : NAN;
+    if (SPLIT && !whole) {
+      const int64_t at = ((int64_t)(sp.q0 + i) * a.heads + hd) * cut.chunks + chunk;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          *reinterpret_cast<f32x4 *>(parts.o + at * D + 64 * v + 16 * j + 4 * x) =
+              f32x4{o[n][v][0][x], o[n][v][1][x], o[n][v][2][x], o[n][v][3][x]};
+      if (j == 0) parts.ml[at] = make_float4(mrun[n], lrun[n], lexact[n], 0.f);
+      continue;
+    }
+    const float inv = inverse(lrun[n]);
     uint16_t *op = a.out + (int64_t)(sp.q0 + i) * a.ost + (int64_t)hd * a.osh + 16 * j;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -323,40 +433,148 @@ rows_kernel(Kv4Attn a, int tiles) {
         for (int x = 0; x < 8; ++x) w[x] = (__bf16)(o[n][v][x & 3][2 * half + (x >> 2)] * inv);
         *reinterpret_cast<bf16x8 *>(op + 64 * v + 8 * half) = w;
       }
-    if (a.lse && j == 0) {
-      // reference, exponent and log2 of the mantissa in fp64: the first two
-      // can be large where the LSE is small
-      const double l2 = (double)mrun[n] + (double)__builtin_amdgcn_frexp_expf(lexact[n]) +
-                        (double)__log2f(__builtin_amdgcn_frexp_mantf(lexact[n]));
-      a.lse[(int64_t)(sp.q0 + i) * a.heads + hd] =
-          lexact[n] > 0.f ? (float)(l2 * 0.69314718055994531) : lexact[n] == 0.f ? -INFINITY : NAN;
-    }
+    if (a.lse && j == 0) a.lse[(int64_t)(sp.q0 + i) * a.heads + hd] = lse_of(mrun[n], lexact[n]);
   }
 }
 
+// Joins the parts of a query row and head, in their order: a wave sums every
+// fourth part, 64 lanes over the channels.
+template <int D>
+__global__ void __launch_bounds__(64 * kWaves)
+join_kernel(Kv4Attn a, Cut cut, Parts parts, int tile_rows) {
+  constexpr int C = D / 64;  // channels of a lane
+  __shared__ float factor[kMaxChunks];
+  __shared__ float sums[kWaves][D];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int id = (int)blockIdx.x;
+  const int hd = id % a.heads;
+  id /= a.heads;
+  const int b = id % a.batch, i = id / a.batch;
+  const Span sp = span_of(a, b);
+  if (i >= min(sp.m, a.max_q)) return;
+  const int row = i * a.group + hd % a.group;
+  const int end = tile_end(a, sp, row - row % tile_rows, tile_rows);
+  if (end <= cut.chunk) return;
+  const int n = (end + cut.chunk - 1) / cut.chunk;
+  const int64_t at = ((int64_t)(sp.q0 + i) * a.heads + hd) * cut.chunks;
+  float m = -INFINITY;
+  for (int c = lane; c < n; c += 64) m = fmaxf(m, parts.ml[at + c].x);
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f, le = 0.f;
+  for (int c = lane; c < n; c += 64) {
+    const float4 x = parts.ml[at + c];
+    const float f = __builtin_amdgcn_exp2f(x.x - ref);
+    if (wave == 0) factor[c] = f;
+    l += x.y * f;
+    le += x.z * f;
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    l += __shfl_xor(l, s);
+    le += __shfl_xor(le, s);
+  }
+  __syncthreads();
+  float o[C] = {};
+#pragma unroll 4
+  for (int c = wave; c < n; c += kWaves) {
+    const float f = factor[c];
+#pragma unroll
+    for (int x = 0; x < C; ++x) o[x] += f * parts.o[(at + c) * D + 64 * x + lane];
+  }
+#pragma unroll
+  for (int x = 0; x < C; ++x) sums[wave][64 * x + lane] = o[x];
+  __syncthreads();
+  if (threadIdx.x < D) {
+    const int c = threadIdx.x;
+    const float v = ((sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c])) * inverse(l);
+    a.out[(int64_t)(sp.q0 + i) * a.ost + (int64_t)hd * a.osh + c] = __builtin_bit_cast(uint16_t, (__bf16)v);
+  }
+  if (a.lse && threadIdx.x == 0) a.lse[(int64_t)(sp.q0 + i) * a.heads + hd] = lse_of(m, le);
+}
+
 template <int D, int NT>
-hipError_t launch_rows(const Kv4Attn &a, hipStream_t s) {
-  const int64_t rows = (int64_t)a.max_q * a.group;
-  const int64_t tiles = (rows + 16 * NT - 1) / (16 * NT);
+hipError_t launch_rows(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s) {
   const size_t lds = (size_t)2 * NT * (D / 64 * 16 + 3) * 64 * 4;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&rows_kernel<D, NT>),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  const int64_t grid = (int64_t)cut.tiles * a.batch * a.c.heads * cut.chunks;
+  const auto f = cut.chunks > 1 ? &rows_kernel<D, NT, true> : &rows_kernel<D, NT, false>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           (int)lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((rows_kernel<D, NT>), dim3((unsigned)(tiles * a.batch * a.c.heads)), dim3(64 * kWaves), lds, s, a,
-                     (int)tiles);
+  hipLaunchKernelGGL(f, dim3((unsigned)grid), dim3(64 * kWaves), lds, s, a, cut, parts);
+  if (cut.chunks > 1)
+    hipLaunchKernelGGL(join_kernel<D>, dim3((unsigned)((int64_t)a.max_q * a.batch * a.heads)), dim3(64 * kWaves), 0, s, a,
+                       cut, parts, 16 * NT);
   return hipGetLastError();
+}
+
+// Row tiles of 16, 32 or 64 rows, whichever hold a request's rows.
+int tile_of(const Kv4Attn &a) {
+  const int64_t rows = (int64_t)a.max_q * a.group;
+  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+}
+
+// Parts of the key axis.  One workgroup takes 0.7 us for its four waves' 128
+// tokens, and three of them fit a CU, so the axis is cut for about 640
+// workgroups; parts of 128 tokens to 1536 (longer ones balance ragged lengths
+// worse and save nothing).  The second kernel costs 3 us: axes of 512 tokens
+// stay whole, those of 1024 where there are more than 64 workgroups.  us at d =
+// 128 with parts of 128 / 256 / 512 / 1024 / 2048 tokens / whole:
+//   8 heads, 512 tokens: 8.5 / 9.3 / - / - / - / 7.3
+//   8 heads, 1024: 8.7 / 9.2 / 10.6 / - / - / 9.9
+//   8 heads, 4096: 9.0 / 9.5 / 10.8 / 13.4 / 18.8 / 26
+//   32 heads, 4096: 13.6 / 11.3 / 11.4 / 13.5 / 18.8 / 26
+//   128 heads, 1024: 15.9 / 12.5 / 12.8 / - / - / 10.1
+//   192 heads, 4096: 39.5 / 30.2 / 26.8 / 25.4 / 27.8 / 30.3
+//   128 heads, 16,384: 121 / 85 / 69 / 57 / 60 / 120
+// The lengths are on the device: the table's width is what the axis may reach.
+Cut cut_of(const Kv4Attn &a) {
+  const int nt = tile_of(a);
+  const int64_t rows = (int64_t)a.max_q * a.group;
+  const int64_t tiles = (rows + 16 * nt - 1) / (16 * nt);
+  const int64_t reach = (int64_t)a.width << a.c.shift;
+  const int64_t base = tiles * a.batch * a.c.heads;
+  Cut cut{(int)tiles, (int)reach, 1};
+  if (tiles > 1 && base >= 512) return cut;  // rows enough; their parts would be much to join
+  if (reach <= 512 || (reach <= 1024 && base > 64)) return cut;
+  const auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+  int64_t chunk = up(up(reach * base, 640), 128) * 128;
+  chunk = chunk > 1536 ? 1536 : chunk;
+  if (chunk * kMaxChunks < reach) chunk = up(reach, kMaxChunks * 128) * 128;
+  cut.chunk = (int)chunk;
+  cut.chunks = (int)up(reach, chunk);
+  return cut;
 }
 
 }  // namespace
 
 int64_t kv4_attn_workgroups(const Kv4Attn &a) {
-  return ((int64_t)a.max_q * a.group + 63) / 64 * a.batch * a.c.heads;
+  const Cut cut = cut_of(a);
+  const int64_t rows = (int64_t)a.max_q * a.batch * a.heads, main = (int64_t)cut.tiles * a.batch * a.c.heads * cut.chunks;
+  return cut.chunks > 1 && rows > main ? rows : main;
 }
 
-size_t kv4_attn_scratch_bytes(const Kv4Attn &) { return 0; }
+// Parts: their outputs, then their references and sums.
+size_t kv4_attn_scratch_bytes(const Kv4Attn &a) {
+  const Cut cut = cut_of(a);
+  if (cut.chunks == 1) return 0;
+  const size_t n = (size_t)a.n_rows * a.heads * cut.chunks;
+  return align_up(n * a.c.d * 4) + align_up(n * 16);
+}
 
-hipError_t launch_kv4_attn(const Kv4Attn &a, void *, hipStream_t s) {
-  return a.c.d == 128 ? launch_rows<128, 4>(a, s) : launch_rows<64, 4>(a, s);
+hipError_t launch_kv4_attn(const Kv4Attn &a, void *scratch, hipStream_t s) {
+  const Cut cut = cut_of(a);
+  Parts parts{static_cast<float *>(scratch), nullptr};
+  if (cut.chunks > 1)
+    parts.ml = reinterpret_cast<float4 *>(static_cast<char *>(scratch) +
+                                          align_up((size_t)a.n_rows * a.heads * cut.chunks * a.c.d * 4));
+  const int nt = tile_of(a);
+  if (a.c.d == 128)
+    return nt == 1 ? launch_rows<128, 1>(a, cut, parts, s)
+                   : nt == 2 ? launch_rows<128, 2>(a, cut, parts, s) : launch_rows<128, 4>(a, cut, parts, s);
+  return nt == 1 ? launch_rows<64, 1>(a, cut, parts, s)
+                 : nt == 2 ? launch_rows<64, 2>(a, cut, parts, s) : launch_rows<64, 4>(a, cut, parts, s);
 }
 
 }  // namespace carnator

@@ -14,85 +14,14 @@
 // are an A operand of V^T each once the two are told apart.  Rows of a K tile
 // are permuted so that the scores of eight consecutive tokens end in one lane,
 // as the B operand of the second product.
-#include "internal.h"
-
-#include <math.h>
+#include "kv4_attn.h"
 
 namespace carnator {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kWaves = 4;
 constexpr int kStep = 32;  // tokens of a wave's step
 constexpr int kAhead = 1;  // steps whose loads are under way
-constexpr int kMaxChunks = 256;
-// Growth of the running maximum (log2 units) below which O and l keep their
-// scale: P may then reach 2^8, harmless in fp32 and bf16.
-constexpr float kSlack = 8.f;
-
-// Two channels (or tokens) of byte SEL of `codes` as bf16, under the exponent
-// bits of `scale` (the conversion reads no other bit of it).
-template <int SEL>
-__device__ inline uint32_t pair_of(uint32_t codes, uint32_t scale) {
-  return __builtin_bit_cast(uint32_t,
-                            __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, __builtin_bit_cast(float, scale), SEL));
-}
-// Eight channels: four bytes under one scale.
-__device__ inline bf16x8 eight_of(uint32_t codes, uint32_t scale) {
-  return __builtin_bit_cast(bf16x8, u32x4{pair_of<0>(codes, scale), pair_of<1>(codes, scale),
-                                          pair_of<2>(codes, scale), pair_of<3>(codes, scale)});
-}
-
-// 1 / l; 0 where nothing was seen.
-__device__ inline float inverse(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN; }
-// Natural log-sum-exp from a reference m (log2 units) and the sum beside it:
-// reference, exponent and log2 of the mantissa are added in fp64, since the
-// first two can be large where the result is small.
-__device__ inline float lse_of(float m, float l) {
-  const double l2 = (double)m + (double)__builtin_amdgcn_frexp_expf(l) + (double)__log2f(__builtin_amdgcn_frexp_mantf(l));
-  return l > 0.f ? (float)(l2 * 0.69314718055994531) : l == 0.f ? -INFINITY : NAN;
-}
-
-// What a request's queries are and see.
-struct Span {
-  int q0;     // first query row
-  int m;      // queries (before max_q), for the causal limit
-  int rows;   // query rows times heads of a cached head
-  int kv;     // tokens
-  __device__ int limit(const Kv4Attn &a, int i) const {  // tokens that query i sees
-    return a.causal ? min(max(kv - m + i + 1, 0), kv) : kv;
-  }
-};
-__device__ inline Span span_of(const Kv4Attn &a, int b) {
-  const int q0 = __builtin_amdgcn_readfirstlane(a.q_start[b]), q1 = __builtin_amdgcn_readfirstlane(a.q_start[b + 1]);
-  const int kv = __builtin_amdgcn_readfirstlane(a.kv_len[b]);
-  Span s;
-  s.q0 = min(max(q0, 0), a.n_rows);
-  s.m = min(max(q1, s.q0), a.n_rows) - s.q0;
-  s.rows = min(s.m, a.max_q) * a.group;
-  s.kv = min(max(kv, 0), a.width << a.c.shift);
-  return s;
-}
-// Tokens that the last of 16 NT rows from row0 on sees: what a tile walks.
-__device__ inline int tile_end(const Kv4Attn &a, const Span &s, int row0, int rows) {
-  return s.limit(a, (min(row0 + rows, s.rows) - 1) / a.group);
-}
-
-// How a call is cut: row tiles, and parts of the key axis of `chunk` tokens
-// whose results a second kernel joins.
-struct Cut {
-  int tiles, chunk, chunks;
-};
-// Results of the parts: outputs [n_rows * heads][chunks][d] not yet divided,
-// (reference, rounded sum, sum) beside them.
-struct Parts {
-  float *o;
-  float4 *ml;
-};
 
 // What a wave reads of 32 tokens.
 template <int D>
@@ -120,7 +49,7 @@ rows_kernel(Kv4Attn a, Cut cut, Parts parts) {
   const int b = id % a.batch, chunk = SPLIT ? id / a.batch : 0;
   const Span sp = span_of(a, b);
   const int row0 = tile * 16 * NT;
-  if (row0 >= sp.rows) return;
+  if (!cut.has(sp) || row0 >= sp.rows) return;
   const int end = tile_end(a, sp, row0, 16 * NT);  // tokens that a row of the tile sees
   const int k_first = SPLIT ? chunk * cut.chunk : 0;
   if (k_first >= end && chunk > 0) return;
@@ -441,7 +370,7 @@ rows_kernel(Kv4Attn a, Cut cut, Parts parts) {
 // fourth part, 64 lanes over the channels.
 template <int D>
 __global__ void __launch_bounds__(64 * kWaves)
-join_kernel(Kv4Attn a, Cut cut, Parts parts, int tile_rows) {
+join_kernel(Kv4Attn a, Cut cut, Parts parts) {
   constexpr int C = D / 64;  // channels of a lane
   __shared__ float factor[kMaxChunks];
   __shared__ float sums[kWaves][D];
@@ -451,9 +380,9 @@ join_kernel(Kv4Attn a, Cut cut, Parts parts, int tile_rows) {
   id /= a.heads;
   const int b = id % a.batch, i = id / a.batch;
   const Span sp = span_of(a, b);
-  if (i >= min(sp.m, a.max_q)) return;
+  if (!cut.has(sp) || i * a.group >= sp.rows) return;
   const int row = i * a.group + hd % a.group;
-  const int end = tile_end(a, sp, row - row % tile_rows, tile_rows);
+  const int end = tile_end(a, sp, row - row % cut.tile_rows, cut.tile_rows);
   if (end <= cut.chunk) return;
   const int n = (end + cut.chunk - 1) / cut.chunk;
   const int64_t at = ((int64_t)(sp.q0 + i) * a.heads + hd) * cut.chunks;
@@ -503,19 +432,24 @@ hipError_t launch_rows(const Kv4Attn &a, const Cut &cut, const Parts &parts, hip
                                            (int)lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(f, dim3((unsigned)grid), dim3(64 * kWaves), lds, s, a, cut, parts);
-  if (cut.chunks > 1)
-    hipLaunchKernelGGL(join_kernel<D>, dim3((unsigned)((int64_t)a.max_q * a.batch * a.heads)), dim3(64 * kWaves), 0, s, a,
-                       cut, parts, 16 * NT);
   return hipGetLastError();
 }
 
-// Row tiles of 16, 32 or 64 rows, whichever hold a request's rows.
-int tile_of(const Kv4Attn &a) {
-  const int64_t rows = (int64_t)a.max_q * a.group;
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
+
+// Rows of a request, at most.
+int64_t most_rows(const Kv4Attn &a) { return (int64_t)a.max_q * a.group; }
+
+constexpr int kFewRows = 64;  // rows of a request up to which rows_kernel takes it
+
+// Cuts the key axis into parts of `chunk` tokens (a multiple of 128).
+void set_chunk(Cut &cut, int64_t reach, int64_t chunk) {
+  if (chunk * kMaxChunks < reach) chunk = up(reach, kMaxChunks * 128) * 128;
+  cut.chunk = (int)chunk;
+  cut.chunks = (int)up(reach, chunk);
 }
 
-// Parts of the key axis.  One workgroup takes 0.7 us for its four waves' 128
+// The requests of few rows.  One workgroup takes 0.7 us for its four waves' 128
 // tokens, and three of them fit a CU, so the axis is cut for about 640
 // workgroups; parts of 128 tokens to 1536 (longer ones balance ragged lengths
 // worse and save nothing).  The second kernel costs 3 us: axes of 512 tokens
@@ -529,52 +463,88 @@ int tile_of(const Kv4Attn &a) {
 //   192 heads, 4096: 39.5 / 30.2 / 26.8 / 25.4 / 27.8 / 30.3
 //   128 heads, 16,384: 121 / 85 / 69 / 57 / 60 / 120
 // The lengths are on the device: the table's width is what the axis may reach.
-Cut cut_of(const Kv4Attn &a) {
-  const int nt = tile_of(a);
-  const int64_t rows = (int64_t)a.max_q * a.group;
-  const int64_t tiles = (rows + 16 * nt - 1) / (16 * nt);
+Cut few_cut(const Kv4Attn &a) {
+  const int64_t rows = most_rows(a) < kFewRows ? most_rows(a) : kFewRows;
+  const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int64_t reach = (int64_t)a.width << a.c.shift;
-  const int64_t base = tiles * a.batch * a.c.heads;
-  Cut cut{(int)tiles, (int)reach, 1};
-  if (tiles > 1 && base >= 512) return cut;  // rows enough; their parts would be much to join
+  const int64_t base = (int64_t)a.batch * a.c.heads;
+  Cut cut{0, kFewRows, 16 * nt, 1, (int)reach, 1};
   if (reach <= 512 || (reach <= 1024 && base > 64)) return cut;
-  const auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
-  int64_t chunk = up(up(reach * base, 640), 128) * 128;
-  chunk = chunk > 1536 ? 1536 : chunk;
-  if (chunk * kMaxChunks < reach) chunk = up(reach, kMaxChunks * 128) * 128;
-  cut.chunk = (int)chunk;
-  cut.chunks = (int)up(reach, chunk);
+  const int64_t chunk = up(up(reach * base, 640), 128) * 128;
+  set_chunk(cut, reach, chunk > 1536 ? 1536 : chunk);
   return cut;
+}
+
+// The requests of more rows (tiles is 0 where there can be none).  Two workgroups
+// fit a CU; parts only for grids that leave CUs empty.
+Cut many_cut(const Kv4Attn &a) {
+  const int64_t reach = (int64_t)a.width << a.c.shift;
+  Cut cut{kFewRows, 0x7FFFFFFF, kTileRows, 0, (int)reach, 1};
+  if (most_rows(a) <= kFewRows) return cut;
+  if (a.batch == 1) cut.over = 0;  // a single request is left to this kernel however few rows it has
+  cut.tiles = (int)up(most_rows(a), kTileRows);
+  const int64_t base = (int64_t)cut.tiles * a.batch * a.c.heads;
+  if (base < 256 && reach > 1024) {
+    const int64_t chunk = up(up(reach * base, 512), 128) * 128;
+    set_chunk(cut, reach, chunk < 512 ? 512 : chunk);
+  }
+  return cut;
+}
+
+// Scratch of a cut: the parts' outputs, then their references and sums.
+size_t outputs_bytes(const Kv4Attn &a, const Cut &cut) {
+  return align_up((size_t)a.n_rows * a.heads * cut.chunks * a.c.d * 4);
+}
+size_t parts_bytes(const Kv4Attn &a, const Cut &cut) {
+  if (cut.chunks == 1 || cut.tiles == 0) return 0;
+  return outputs_bytes(a, cut) + align_up((size_t)a.n_rows * a.heads * cut.chunks * 16);
+}
+int64_t workgroups(const Kv4Attn &a, const Cut &cut) {
+  const int64_t main = (int64_t)cut.tiles * a.batch * a.c.heads * cut.chunks;
+  const int64_t join = cut.chunks > 1 ? (int64_t)a.max_q * a.batch * a.heads : 0;
+  return main > join ? main : join;
+}
+Parts parts_at(const Kv4Attn &a, const Cut &cut, char *at) {
+  return Parts{reinterpret_cast<float *>(at), reinterpret_cast<float4 *>(at + outputs_bytes(a, cut))};
+}
+
+hipError_t launch_join(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s) {
+  // rows of the requests that it joins
+  const int64_t most = cut.upto < most_rows(a) ? cut.upto / a.group : a.max_q;
+  const dim3 grid((unsigned)(most * a.batch * a.heads));
+  if (a.c.d == 128) hipLaunchKernelGGL(join_kernel<128>, grid, dim3(64 * kWaves), 0, s, a, cut, parts);
+  else hipLaunchKernelGGL(join_kernel<64>, grid, dim3(64 * kWaves), 0, s, a, cut, parts);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t kv4_attn_workgroups(const Kv4Attn &a) {
-  const Cut cut = cut_of(a);
-  const int64_t rows = (int64_t)a.max_q * a.batch * a.heads, main = (int64_t)cut.tiles * a.batch * a.c.heads * cut.chunks;
-  return cut.chunks > 1 && rows > main ? rows : main;
+  const int64_t x = workgroups(a, few_cut(a)), y = workgroups(a, many_cut(a));
+  return x > y ? x : y;
 }
 
-// Parts: their outputs, then their references and sums.
-size_t kv4_attn_scratch_bytes(const Kv4Attn &a) {
-  const Cut cut = cut_of(a);
-  if (cut.chunks == 1) return 0;
-  const size_t n = (size_t)a.n_rows * a.heads * cut.chunks;
-  return align_up(n * a.c.d * 4) + align_up(n * 16);
-}
+size_t kv4_attn_scratch_bytes(const Kv4Attn &a) { return parts_bytes(a, few_cut(a)) + parts_bytes(a, many_cut(a)); }
 
 hipError_t launch_kv4_attn(const Kv4Attn &a, void *scratch, hipStream_t s) {
-  const Cut cut = cut_of(a);
-  Parts parts{static_cast<float *>(scratch), nullptr};
-  if (cut.chunks > 1)
-    parts.ml = reinterpret_cast<float4 *>(static_cast<char *>(scratch) +
-                                          align_up((size_t)a.n_rows * a.heads * cut.chunks * a.c.d * 4));
-  const int nt = tile_of(a);
-  if (a.c.d == 128)
-    return nt == 1 ? launch_rows<128, 1>(a, cut, parts, s)
-                   : nt == 2 ? launch_rows<128, 2>(a, cut, parts, s) : launch_rows<128, 4>(a, cut, parts, s);
-  return nt == 1 ? launch_rows<64, 1>(a, cut, parts, s)
-                 : nt == 2 ? launch_rows<64, 2>(a, cut, parts, s) : launch_rows<64, 4>(a, cut, parts, s);
+  const Cut few = few_cut(a), many = many_cut(a);
+  char *at = static_cast<char *>(scratch);
+  hipError_t e = hipSuccess;
+  if (many.tiles > 0) {
+    const Parts parts = parts_at(a, many, at + parts_bytes(a, few));
+    if ((e = launch_kv4_tiles(a, many, parts, s)) != hipSuccess) return e;
+    if (many.chunks > 1 && (e = launch_join(a, many, parts, s)) != hipSuccess) return e;
+    if (many.over == 0) return e;
+  }
+  const Parts parts = parts_at(a, few, at);
+  const bool d128 = a.c.d == 128;
+  switch (few.tile_rows) {
+    case 16: e = d128 ? launch_rows<128, 1>(a, few, parts, s) : launch_rows<64, 1>(a, few, parts, s); break;
+    case 32: e = d128 ? launch_rows<128, 2>(a, few, parts, s) : launch_rows<64, 2>(a, few, parts, s); break;
+    default: e = d128 ? launch_rows<128, 4>(a, few, parts, s) : launch_rows<64, 4>(a, few, parts, s);
+  }
+  if (e != hipSuccess || few.chunks == 1) return e;
+  return launch_join(a, few, parts, s);
 }
 
 }  // namespace carnator

@@ -21,7 +21,6 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kStep = 32;  // tokens of a wave's step
-constexpr int kAhead = 1;  // steps whose loads are under way
 
 // What a wave reads of 32 tokens.
 template <int D>
@@ -261,26 +260,22 @@ rows_kernel(Kv4Attn a, Cut cut, Parts parts) {
       }
     }
   };
-  // the loads of kAhead steps are under way during a step
-  constexpr int NB = kAhead + 1;
-  Raw<D> buf[NB];
-  int at[NB], last = k_first + (wave - kWaves) * kStep;
-  auto fetch = [&](int slot) {
-    at[slot] = last = next(last + kWaves * kStep);
-    if (last < k_end) load(buf[slot], last);
-  };
-#pragma unroll
-  for (int s = 0; s < kAhead; ++s) fetch(s);
-  for (bool more = true; more;) {
-#pragma unroll
-    for (int s = 0; s < NB; ++s) {
-      if (at[s] >= k_end) {
-        more = false;
-        break;
-      }
-      fetch((s + kAhead) % NB);
-      step(buf[s], at[s]);
+  // the loads of a step are under way during the one before
+  Raw<D> even, odd;
+  const int stride = kWaves * kStep;
+  int k0 = next(k_first + wave * kStep);
+  if (k0 < k_end) {
+    load(even, k0);
+    int k1 = next(k0 + stride);
+    while (k1 < k_end) {
+      load(odd, k1);
+      step(even, k0);
+      k0 = next(k1 + stride);
+      if (k0 < k_end) load(even, k0);
+      step(odd, k1);
+      k1 = next(k0 + stride);
     }
+    if (k0 < k_end) step(even, k0);
   }
   // ---- sums over the lanes of a query, then the waves' parts in a fixed order
 #pragma unroll
@@ -423,6 +418,51 @@ join_kernel(Kv4Attn a, Cut cut, Parts parts) {
   if (a.lse && threadIdx.x == 0) a.lse[(int64_t)(sp.q0 + i) * a.heads + hd] = lse_of(m, le);
 }
 
+// The same for few parts of many rows: D / 4 lanes take a query row and head, and
+// no lane waits for another.
+template <int D>
+__global__ void __launch_bounds__(256)
+join_few_kernel(Kv4Attn a, Cut cut, Parts parts, int most) {
+  constexpr int LANES = D / 4;
+  int64_t id = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  const int c4 = 4 * (threadIdx.x % LANES);
+  const int hd = (int)(id % a.heads);
+  id /= a.heads;
+  const int i = (int)(id % most), b = (int)(id / most);
+  if (b >= a.batch) return;
+  Span sp;  // of this lane's request (a workgroup may hold rows of two)
+  sp.q0 = min(max(a.q_start[b], 0), a.n_rows);
+  sp.m = min(max(a.q_start[b + 1], sp.q0), a.n_rows) - sp.q0;
+  sp.rows = min(sp.m, a.max_q) * a.group;
+  sp.kv = min(max(a.kv_len[b], 0), a.width << a.c.shift);
+  if (!cut.has(sp) || i * a.group >= sp.rows) return;
+  const int row = i * a.group + hd % a.group;
+  const int end = tile_end(a, sp, row - row % cut.tile_rows, cut.tile_rows);
+  if (end <= cut.chunk) return;
+  const int n = (end + cut.chunk - 1) / cut.chunk;
+  const int64_t at = ((int64_t)(sp.q0 + i) * a.heads + hd) * cut.chunks;
+  float m = -INFINITY;
+  for (int c = 0; c < n; ++c) m = fmaxf(m, parts.ml[at + c].x);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f, le = 0.f;
+  f32x4 o = {};
+#pragma unroll 4
+  for (int c = 0; c < n; ++c) {
+    const float4 x = parts.ml[at + c];
+    const f32x4 v = *reinterpret_cast<const f32x4 *>(parts.o + (at + c) * D + c4);
+    const float f = __builtin_amdgcn_exp2f(x.x - ref);
+    l += x.y * f;
+    le += x.z * f;
+    o += v * f;
+  }
+  const float inv = inverse(l);
+  bf16x4 w;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) w[x] = (__bf16)(o[x] * inv);
+  *reinterpret_cast<bf16x4 *>(a.out + (int64_t)(sp.q0 + i) * a.ost + (int64_t)hd * a.osh + c4) = w;
+  if (a.lse && c4 == 0) a.lse[(int64_t)(sp.q0 + i) * a.heads + hd] = lse_of(m, le);
+}
+
 template <int D, int NT>
 hipError_t launch_rows(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s) {
   const size_t lds = (size_t)2 * NT * (D / 64 * 16 + 3) * 64 * 4;
@@ -435,12 +475,17 @@ hipError_t launch_rows(const Kv4Attn &a, const Cut &cut, const Parts &parts, hip
   return hipGetLastError();
 }
 
+constexpr int kMaxParts = 64;  // parts of the requests of many rows
+
 int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
 
 // Rows of a request, at most.
 int64_t most_rows(const Kv4Attn &a) { return (int64_t)a.max_q * a.group; }
 
-constexpr int kFewRows = 64;  // rows of a request up to which rows_kernel takes it
+// Rows of a request up to which rows_kernel takes it: at d = 128 the outputs of
+// 64 rows do not fit the registers of two waves a SIMD (8 heads, 16,000 tokens,
+// 48 rows: 35 us with one wave a SIMD, 23 in the other kernel).
+int few_rows(const Kv4Attn &a) { return a.c.d == 128 ? 32 : 64; }
 
 // Cuts the key axis into parts of `chunk` tokens (a multiple of 128).
 void set_chunk(Cut &cut, int64_t reach, int64_t chunk) {
@@ -464,29 +509,51 @@ void set_chunk(Cut &cut, int64_t reach, int64_t chunk) {
 //   128 heads, 16,384: 121 / 85 / 69 / 57 / 60 / 120
 // The lengths are on the device: the table's width is what the axis may reach.
 Cut few_cut(const Kv4Attn &a) {
-  const int64_t rows = most_rows(a) < kFewRows ? most_rows(a) : kFewRows;
+  const int64_t rows = most_rows(a) < few_rows(a) ? most_rows(a) : few_rows(a);
   const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int64_t reach = (int64_t)a.width << a.c.shift;
   const int64_t base = (int64_t)a.batch * a.c.heads;
-  Cut cut{0, kFewRows, 16 * nt, 1, (int)reach, 1};
+  Cut cut{0, few_rows(a), 16 * nt, 1, (int)reach, 1};
   if (reach <= 512 || (reach <= 1024 && base > 64)) return cut;
   const int64_t chunk = up(up(reach * base, 640), 128) * 128;
   set_chunk(cut, reach, chunk > 1536 ? 1536 : chunk);
   return cut;
 }
 
-// The requests of more rows (tiles is 0 where there can be none).  Two workgroups
-// fit a CU; parts only for grids that leave CUs empty.
+// The requests of more rows (tiles is 0 where there can be none).  Parts of the
+// key axis fill CUs that the tiles leave empty and even out the last round, and
+// cost their outputs' way through memory; their number is the one with the least
+// time by this: a token of a tile takes 27 ns (19 at d = 64) with two workgroups
+// on the CU and 20 (14.6) with one, so 512 workgroups are a round
+// (half a one more than their number says, past two); a part of a
+// tile adds 0.03 us (half at d = 64) to the joining, which begins at 6 us.  Per call at d =
+// 128, whole / in parts of 512 / 2048 / 4096 tokens:
+//   8 tiles, 2000 tokens: 50 / 25 / - / - us (17 in parts of 128)
+//   60 tiles, 16,000: 317 / 109 / 86 / 103
+//   192 tiles, 16,000: 319 / 325 / 238 / 240
+//   444 tiles, 32,000: 863 / 1416 / 984 / 931
 Cut many_cut(const Kv4Attn &a) {
   const int64_t reach = (int64_t)a.width << a.c.shift;
-  Cut cut{kFewRows, 0x7FFFFFFF, kTileRows, 0, (int)reach, 1};
-  if (most_rows(a) <= kFewRows) return cut;
+  Cut cut{few_rows(a), 0x7FFFFFFF, kTileRows, 0, (int)reach, 1};
+  if (most_rows(a) <= few_rows(a)) return cut;
   if (a.batch == 1) cut.over = 0;  // a single request is left to this kernel however few rows it has
   cut.tiles = (int)up(most_rows(a), kTileRows);
-  const int64_t base = (int64_t)cut.tiles * a.batch * a.c.heads;
-  if (base < 256 && reach > 1024) {
-    const int64_t chunk = up(up(reach * base, 512), 128) * 128;
-    set_chunk(cut, reach, chunk < 512 ? 512 : chunk);
+  // tiles that hold rows, about: the requests' sum is at most n_rows
+  const int64_t all = (int64_t)cut.tiles * a.batch, held = up((int64_t)a.n_rows * a.group, kTileRows);
+  const int64_t base = (all < held ? all : held) * a.c.heads;
+  const double two = a.c.d == 128 ? 0.027 : 0.019, one = a.c.d == 128 ? 0.020 : 0.0146;
+  const double part = a.c.d == 128 ? 0.03 : 0.015;
+  double best = 1e300;
+  for (int64_t n = 1; n <= kMaxParts && (n == 1 || reach >= n * 128); ++n) {
+    const int64_t chunk = n == 1 ? reach : up(up(reach, n), 128) * 128;
+    const double rounds = base * n <= 256 ? one / two : base * n <= 1024 ? (double)up(base * n, 512)
+                                                                         : (double)(base * n) / 512 + 0.5;
+    const double us = rounds * two * (double)chunk + (n > 1 ? 6 + part * (double)(base * n) : 0);
+    if (us < best) {
+      best = us;
+      cut.chunk = (int)chunk;
+      cut.chunks = (int)up(reach, chunk);
+    }
   }
   return cut;
 }
@@ -510,10 +577,18 @@ Parts parts_at(const Kv4Attn &a, const Cut &cut, char *at) {
 
 hipError_t launch_join(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s) {
   // rows of the requests that it joins
-  const int64_t most = cut.upto < most_rows(a) ? cut.upto / a.group : a.max_q;
-  const dim3 grid((unsigned)(most * a.batch * a.heads));
-  if (a.c.d == 128) hipLaunchKernelGGL(join_kernel<128>, grid, dim3(64 * kWaves), 0, s, a, cut, parts);
-  else hipLaunchKernelGGL(join_kernel<64>, grid, dim3(64 * kWaves), 0, s, a, cut, parts);
+  const int most = cut.upto < most_rows(a) ? cut.upto / a.group : a.max_q;
+  const int64_t n = (int64_t)most * a.batch * a.heads;
+  const bool d128 = a.c.d == 128;
+  if (cut.chunks <= 16 && n >= 2048) {
+    const dim3 grid((unsigned)up(n, 1024 / a.c.d));
+    if (d128) hipLaunchKernelGGL(join_few_kernel<128>, grid, dim3(256), 0, s, a, cut, parts, most);
+    else hipLaunchKernelGGL(join_few_kernel<64>, grid, dim3(256), 0, s, a, cut, parts, most);
+  } else if (d128) {
+    hipLaunchKernelGGL(join_kernel<128>, dim3((unsigned)n), dim3(64 * kWaves), 0, s, a, cut, parts);
+  } else {
+    hipLaunchKernelGGL(join_kernel<64>, dim3((unsigned)n), dim3(64 * kWaves), 0, s, a, cut, parts);
+  }
   return hipGetLastError();
 }
 
@@ -541,7 +616,7 @@ hipError_t launch_kv4_attn(const Kv4Attn &a, void *scratch, hipStream_t s) {
   switch (few.tile_rows) {
     case 16: e = d128 ? launch_rows<128, 1>(a, few, parts, s) : launch_rows<64, 1>(a, few, parts, s); break;
     case 32: e = d128 ? launch_rows<128, 2>(a, few, parts, s) : launch_rows<64, 2>(a, few, parts, s); break;
-    default: e = d128 ? launch_rows<128, 4>(a, few, parts, s) : launch_rows<64, 4>(a, few, parts, s);
+    default: e = launch_rows<64, 4>(a, few, parts, s);
   }
   if (e != hipSuccess || few.chunks == 1) return e;
   return launch_join(a, few, parts, s);

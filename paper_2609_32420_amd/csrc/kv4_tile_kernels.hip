@@ -71,13 +71,18 @@ tile_kernel(Kv4Attn a, Cut cut, Parts parts) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, hh = lane >> 5;
-  // the tiles that see most first; tiles of a head side by side on the grid
-  int id = (int)blockIdx.x;
+  // The tiles that see most first.  Workgroups go to the eight XCDs in turn, so
+  // the heads, requests and parts of a tile are rotated from tile to tile where
+  // their number is even: otherwise the long ones of a ragged batch, or the early
+  // parts of a causal one, would all meet on a few XCDs.
+  const int group = a.c.heads * a.batch * cut.chunks;
+  const int turn_of = (int)blockIdx.x / group;
+  int id = (int)blockIdx.x - turn_of * group;
+  if (group % 2 == 0) id = (id + turn_of) % group;
+  const int tile = cut.tiles - 1 - turn_of;
   const int h = id % a.c.heads;
   id /= a.c.heads;
-  const int b = id % a.batch;
-  id /= a.batch;
-  const int chunk = id % cut.chunks, tile = cut.tiles - 1 - id / cut.chunks;
+  const int b = id % a.batch, chunk = id / a.batch;
   const Span sp = span_of(a, b);
   const int row0 = tile * ROWS;
   if (!cut.has(sp) || row0 >= sp.rows) return;

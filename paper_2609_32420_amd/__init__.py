@@ -673,10 +673,13 @@ def _rows(t: torch.Tensor, name: str, heads: int, d: int, device) -> Rows:
     return Rows(t.data_ptr(), st, sh)
 
 
+_INT32 = torch.int32
+
+
 def _i32(t: torch.Tensor, name: str, shape, device) -> int:
-    if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous int32 tensor %s on %s" % (name, list(shape), device))
-    return t.data_ptr()
+    if t.dtype is _INT32 and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError("%s must be a contiguous int32 tensor %s on %s" % (name, list(shape), device))
 
 
 def _call(f, device, *args):
@@ -710,7 +713,9 @@ def page_plan(kv_len: torch.Tensor, new_len: torch.Tensor, table: torch.Tensor, 
     if out is None:
         if n_slots < 0:
             raise ValueError("n_slots must be >= 0")
-        out = [torch.empty(n, dtype=torch.int32, device=dev) for n in (B + 1, B, n_slots, n_slots, 3)]
+        # one allocation for the five
+        out = torch.empty(2 * (B + n_slots) + 4, dtype=torch.int32, device=dev).split((n_slots, n_slots, B + 1, B, 3))
+        out = (out[2], out[3], out[0], out[1], out[4])
     q_start, kv_out, slots, positions, counts = out
     _call(lib().carnator_page_plan, dev, _i32(kv_len, "kv_len", (B,), dev), _i32(new_len, "new_len", (B,), dev), B,
           _i32(table, "table", (B, W), dev), W, _i32(free_pages, "free_pages", (free_pages.shape[0],), dev),

@@ -186,6 +186,12 @@ hipError_t launch_bsattn(View q, View k, View v, uint16_t *out, int64_t osb, int
                          const int32_t *col_idx, const int32_t *order, const int32_t *n_rows,
                          float scale, float *lse, hipStream_t s);
 
+// Dynamic LDS past 64 KB has to be asked for (each time: nothing is remembered).
+inline hipError_t allow_lds(const void *kernel, size_t bytes) {
+  if (bytes <= 65536) return hipSuccess;
+  return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
 // ---- 4-bit cached keys and values ----------------------------------------------
 // Pages of 64 or 128 tokens (block = 1 << shift), the format of include/carnator.h.
 struct Kv4 {

@@ -468,8 +468,7 @@ hipError_t launch_rows(const Kv4Attn &a, const Cut &cut, const Parts &parts, hip
   const size_t lds = (size_t)2 * NT * (D / 64 * 16 + 3) * 64 * 4;
   const int64_t grid = (int64_t)cut.tiles * a.batch * a.c.heads * cut.chunks;
   const auto f = cut.chunks > 1 ? &rows_kernel<D, NT, true> : &rows_kernel<D, NT, false>;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                           (int)lds);
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(f), lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(f, dim3((unsigned)grid), dim3(64 * kWaves), lds, s, a, cut, parts);
   return hipGetLastError();

@@ -412,8 +412,7 @@ hipError_t launch_page_plan(const int32_t *kv_len, const int32_t *new_len, int b
   const bool small = batch <= 256 && n_slots <= 4096;
   const auto f = small ? &plan_kernel<256, 1> : &plan_kernel<1024, 4>;
   const int threads = small ? 256 : 1024;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(f), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                           (kMaxPlanBatch * 2 + 1) * 4);
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(f), lds);
   if (e != hipSuccess) return e;
   const int64_t need = ((int64_t)n_slots + threads * kPlanSlots - 1) / (threads * kPlanSlots);
   const unsigned grid = (unsigned)(need < 1 ? 1 : need > 512 ? 512 : need);

@@ -487,8 +487,7 @@ tile_kernel(Kv4Attn a, Cut cut, Parts parts) {
 template <int D, int WAVES>
 hipError_t launch(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s) {
   using C = TileCfg<D, WAVES>;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&tile_kernel<D, WAVES>),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(&tile_kernel<D, WAVES>), C::LDS);
   if (e != hipSuccess) return e;
   const int64_t grid = (int64_t)cut.tiles * a.batch * a.c.heads * cut.chunks;
   hipLaunchKernelGGL((tile_kernel<D, WAVES>), dim3((unsigned)grid), dim3(C::THREADS), C::LDS, s, a, cut, parts);

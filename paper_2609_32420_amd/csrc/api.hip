@@ -712,6 +712,7 @@ int carnator_kv4_attn(const carnator_rows *q, int32_t n_rows, int32_t heads, con
   if (misaligned4({table, q_start, kv_len, lse}))
     return fail(CARNATOR_E_ALIGN, "table, q_start, kv_len and lse must be 4-byte aligned");
   Kv4Attn a = attn_of(cache, heads, n_rows, batch, width, max_q);
+  a.causal = causal != 0;
   if (kv4_attn_workgroups(a) > kMaxWorkgroups)
     return fail(CARNATOR_E_UNSUPPORTED, "batch * kv_heads * max_q needs %lld workgroups; at most %lld",
                 (long long)kv4_attn_workgroups(a), (long long)kMaxWorkgroups);
@@ -720,7 +721,6 @@ int carnator_kv4_attn(const carnator_rows *q, int32_t n_rows, int32_t heads, con
   a.table = table;
   a.q_start = q_start;
   a.kv_len = kv_len;
-  a.causal = causal != 0;
   a.c2 = (scale > 0.f ? scale : (float)(1.0 / sqrt((double)cache->head_dim))) * 1.4426950408889634f;
   a.out = static_cast<uint16_t *>(out);
   a.ost = ost;

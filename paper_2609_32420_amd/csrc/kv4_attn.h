@@ -72,6 +72,7 @@ __device__ inline int tile_end(const Kv4Attn &a, const Span &s, int row0, int ro
 struct Cut {
   int over, upto;
   int tile_rows, tiles, chunk, chunks;
+  int turns;  // of the grid of the kernel for many rows
   __device__ bool has(const Span &s) const { return s.rows > over && s.rows <= upto; }
 };
 // Results of the parts: outputs [n_rows * heads][chunks][d] not yet divided,

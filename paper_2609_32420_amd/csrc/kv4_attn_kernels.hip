@@ -512,7 +512,7 @@ Cut few_cut(const Kv4Attn &a) {
   const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int64_t reach = (int64_t)a.width << a.c.shift;
   const int64_t base = (int64_t)a.batch * a.c.heads;
-  Cut cut{0, few_rows(a), 16 * nt, 1, (int)reach, 1};
+  Cut cut{0, few_rows(a), 16 * nt, 1, (int)reach, 1, 1};
   if (reach <= 512 || (reach <= 1024 && base > 64)) return cut;
   const int64_t chunk = up(up(reach * base, 640), 128) * 128;
   set_chunk(cut, reach, chunk > 1536 ? 1536 : chunk);
@@ -533,7 +533,7 @@ Cut few_cut(const Kv4Attn &a) {
 //   444 tiles, 32,000: 863 / 1416 / 984 / 931
 Cut many_cut(const Kv4Attn &a) {
   const int64_t reach = (int64_t)a.width << a.c.shift;
-  Cut cut{few_rows(a), 0x7FFFFFFF, kTileRows, 0, (int)reach, 1};
+  Cut cut{few_rows(a), 0x7FFFFFFF, kTileRows, 0, (int)reach, 1, 0};
   if (most_rows(a) <= few_rows(a)) return cut;
   if (a.batch == 1) cut.over = 0;  // a single request is left to this kernel however few rows it has
   cut.tiles = (int)up(most_rows(a), kTileRows);
@@ -554,6 +554,9 @@ Cut many_cut(const Kv4Attn &a) {
       cut.chunks = (int)up(reach, chunk);
     }
   }
+  cut.turns = cut.tiles;
+  if (a.causal && a.batch > 1 && reach * a.group <= 4 * most_rows(a))
+    cut.turns += (int)(reach * a.group / kTileRows);
   return cut;
 }
 
@@ -566,7 +569,7 @@ size_t parts_bytes(const Kv4Attn &a, const Cut &cut) {
   return outputs_bytes(a, cut) + align_up((size_t)a.n_rows * a.heads * cut.chunks * 16);
 }
 int64_t workgroups(const Kv4Attn &a, const Cut &cut) {
-  const int64_t main = (int64_t)cut.tiles * a.batch * a.c.heads * cut.chunks;
+  const int64_t main = (int64_t)cut.turns * a.batch * a.c.heads * cut.chunks;
   const int64_t join = cut.chunks > 1 ? (int64_t)a.max_q * a.batch * a.heads : 0;
   return main > join ? main : join;
 }

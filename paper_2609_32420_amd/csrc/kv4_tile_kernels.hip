@@ -79,13 +79,16 @@ tile_kernel(Kv4Attn a, Cut cut, Parts parts) {
   const int turn_of = (int)blockIdx.x / group;
   int id = (int)blockIdx.x - turn_of * group;
   if (group % 2 == 0) id = (id + turn_of) % group;
-  const int tile = cut.tiles - 1 - turn_of;
   const int h = id % a.c.heads;
   id /= a.c.heads;
   const int b = id % a.batch, chunk = id / a.batch;
   const Span sp = span_of(a, b);
+  // a causal batch by what the tiles see: the tiles of a request that ends
+  // `late` tiles' tokens before the table does are that much later
+  const int late = cut.turns > cut.tiles ? (int)((int64_t)((a.width << a.c.shift) - sp.kv) * a.group / ROWS) : 0;
+  const int tile = (sp.rows + ROWS - 1) / ROWS - 1 - (turn_of - late);
   const int row0 = tile * ROWS;
-  if (!cut.has(sp) || row0 >= sp.rows) return;
+  if (!cut.has(sp) || turn_of < late || tile < 0) return;
   const int end = tile_end(a, sp, row0, ROWS);
   const int k_first = chunk * cut.chunk;
   if (k_first >= end && chunk > 0) return;
@@ -489,7 +492,7 @@ hipError_t launch(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStrea
   using C = TileCfg<D, WAVES>;
   const hipError_t e = allow_lds(reinterpret_cast<const void *>(&tile_kernel<D, WAVES>), C::LDS);
   if (e != hipSuccess) return e;
-  const int64_t grid = (int64_t)cut.tiles * a.batch * a.c.heads * cut.chunks;
+  const int64_t grid = (int64_t)cut.turns * a.batch * a.c.heads * cut.chunks;
   hipLaunchKernelGGL((tile_kernel<D, WAVES>), dim3((unsigned)grid), dim3(C::THREADS), C::LDS, s, a, cut, parts);
   return hipGetLastError();
 }

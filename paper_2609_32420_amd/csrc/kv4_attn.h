@@ -82,8 +82,10 @@ struct Parts {
   float4 *ml;
 };
 
-// The kernel for many rows (kv4_tile_kernels.hip), without the joining.
+// The kernel for many rows (kv4_tile_kernels.hip), without the joining; its last
+// few_groups workgroups take the batch's requests of few rows.
 constexpr int kTileRows = 128;
-hipError_t launch_kv4_tiles(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s);
+hipError_t launch_kv4_tiles(const Kv4Attn &a, const Cut &few, const Parts &few_parts, int few_groups, const Cut &cut,
+                            const Parts &parts, hipStream_t s);
 
 }  // namespace carnator

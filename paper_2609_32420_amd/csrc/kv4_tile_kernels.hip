@@ -16,7 +16,7 @@
 // += V(j-1)^T P(j-1)^T beside the maximum and half of the exponentials of S(j),
 // then S(j+1) beside the other half and beside the conversion of K(j+2) and
 // V(j), whose bytes were loaded during the iteration before.
-#include "kv4_attn.h"
+#include "kv4_rows.h"
 
 #include <math.h>
 
@@ -58,25 +58,33 @@ struct TileCfg {
   static constexpr int RB = 2 * D;               // bytes of a K row
   static constexpr int TB = kKeys * RB;          // a converted tile of K or V
   static constexpr int POISON = 4 * TB;          // K slots 0, 1; V slots 0, 1; then token masks
-  static constexpr int LDS = POISON + 2 * (D / 32) * 8;
+  static constexpr int NT = D == 128 ? 2 : 4;    // tiles of rows_body in the same workgroups
+  static constexpr int OWN = POISON + 2 * (D / 32) * 8;
+  static constexpr int LDS = OWN > rows_lds(D, NT) ? OWN : rows_lds(D, NT);
   static_assert(UNITS >= 1, "a thread converts at least a unit");
+  static_assert(WAVES == kWaves, "rows_body runs in the same workgroups");
 };
 
 template <int D, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2)
-tile_kernel(Kv4Attn a, Cut cut, Parts parts) {
+tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
   using C = TileCfg<D, WAVES>;
   constexpr int UN = C::UNITS;
   constexpr int ROWS = 32 * WAVES;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  const int group = a.c.heads * a.batch * cut.chunks;
+  const int turn_of = (int)blockIdx.x / group;
+  if (turn_of >= cut.turns) {  // requests of few rows (a launch of their own would cost more than they)
+    rows_body<D, C::NT, true>(a, few, few_parts, (int)blockIdx.x - cut.turns * group,
+                                         reinterpret_cast<float *>(lds));
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, hh = lane >> 5;
   // The tiles that see most first.  Workgroups go to the eight XCDs in turn, so
   // the heads, requests and parts of a tile are rotated from tile to tile where
   // their number is even: otherwise the long ones of a ragged batch, or the early
   // parts of a causal one, would all meet on a few XCDs.
-  const int group = a.c.heads * a.batch * cut.chunks;
-  const int turn_of = (int)blockIdx.x / group;
   int id = (int)blockIdx.x - turn_of * group;
   if (group % 2 == 0) id = (id + turn_of) % group;
   const int h = id % a.c.heads;
@@ -488,19 +496,22 @@ tile_kernel(Kv4Attn a, Cut cut, Parts parts) {
 }
 
 template <int D, int WAVES>
-hipError_t launch(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s) {
+hipError_t launch(const Kv4Attn &a, const Cut &few, const Parts &few_parts, int few_groups, const Cut &cut,
+                  const Parts &parts, hipStream_t s) {
   using C = TileCfg<D, WAVES>;
   const hipError_t e = allow_lds(reinterpret_cast<const void *>(&tile_kernel<D, WAVES>), C::LDS);
   if (e != hipSuccess) return e;
-  const int64_t grid = (int64_t)cut.turns * a.batch * a.c.heads * cut.chunks;
-  hipLaunchKernelGGL((tile_kernel<D, WAVES>), dim3((unsigned)grid), dim3(C::THREADS), C::LDS, s, a, cut, parts);
+  const int64_t grid = (int64_t)cut.turns * a.batch * a.c.heads * cut.chunks + few_groups;
+  hipLaunchKernelGGL((tile_kernel<D, WAVES>), dim3((unsigned)grid), dim3(C::THREADS), C::LDS, s, a, few, few_parts, cut, parts);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_kv4_tiles(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s) {
-  return a.c.d == 128 ? launch<128, 4>(a, cut, parts, s) : launch<64, 4>(a, cut, parts, s);
+hipError_t launch_kv4_tiles(const Kv4Attn &a, const Cut &few, const Parts &few_parts, int few_groups, const Cut &cut,
+                            const Parts &parts, hipStream_t s) {
+  return a.c.d == 128 ? launch<128, 4>(a, few, few_parts, few_groups, cut, parts, s)
+                      : launch<64, 4>(a, few, few_parts, few_groups, cut, parts, s);
 }
 
 }  // namespace carnator

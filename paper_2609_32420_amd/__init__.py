@@ -655,7 +655,7 @@ def kv4_pool(n_pages: int, kv_heads: int, head_dim: int, block: int, device="cud
 
 
 def _kv4(pool: torch.Tensor, block: int) -> Kv4:
-    if pool.dim() != 3 or pool.dtype != torch.uint8 or not pool.is_cuda or not pool.is_contiguous():
+    if pool.dtype is not torch.uint8 or pool.dim() != 3 or not pool.is_cuda or not pool.is_contiguous():
         raise ValueError("pool must be a contiguous uint8 CUDA tensor [n_pages, kv_heads, block * d * 17 / 16]")
     n_pages, heads, size = pool.shape
     d = size * 16 // (17 * block)
@@ -664,13 +664,16 @@ def _kv4(pool: torch.Tensor, block: int) -> Kv4:
     return Kv4(pool.data_ptr(), n_pages, heads, d, block)
 
 
+def _is_rows(t: torch.Tensor, heads: int, d: int, device) -> bool:
+    return (t.dtype is torch.bfloat16 and t.dim() == 3 and t.shape[1:] == (heads, d) and t.device == device
+            and t.stride(2) == 1)
+
+
 def _rows(t: torch.Tensor, name: str, heads: int, d: int, device) -> Rows:
-    if t.dim() != 3 or t.dtype != torch.bfloat16 or t.device != device or t.shape[1] != heads or t.shape[2] != d:
-        raise ValueError("%s must be a bf16 tensor [rows, %d, %d] on %s" % (name, heads, d, device))
-    st, sh, sd = t.stride()
-    if sd != 1:
-        raise ValueError("%s must be contiguous along its channels" % name)
-    return Rows(t.data_ptr(), st, sh)
+    if not _is_rows(t, heads, d, device):
+        raise ValueError("%s must be a bf16 tensor [rows, %d, %d] on %s, contiguous along its channels"
+                         % (name, heads, d, device))
+    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
 
 
 _INT32 = torch.int32
@@ -686,10 +689,12 @@ def _call(f, device, *args):
     """A library call with its device as the current one."""
     index = device.index
     if torch._C._cuda_getDevice() == index:
-        _check(f(*args, torch._C._cuda_getCurrentRawStream(index)))
+        status = f(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
         with torch.cuda.device(index):
-            _check(f(*args, torch._C._cuda_getCurrentRawStream(index)))
+            status = f(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        _check(status)
 
 
 def page_plan(kv_len: torch.Tensor, new_len: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor, block: int,
@@ -756,11 +761,10 @@ def kv4_load(pool: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, bloc
         out = tuple(torch.zeros(B, c.kv_heads, n, c.head_dim, dtype=torch.bfloat16, device=dev) for _ in range(2))
     k, v = out
     n = k.shape[2] if n is None and k.dim() == 4 else n
-    for t, name in ((k, "k"), (v, "v")):
-        if (tuple(t.shape) != (B, c.kv_heads, n, c.head_dim) or t.dtype != torch.bfloat16 or t.device != dev
-                or t.stride(3) != 1):
-            raise ValueError("%s must be a bf16 tensor %s on %s, contiguous along its channels"
-                             % (name, [B, c.kv_heads, n, c.head_dim], dev))
+    shape = (B, c.kv_heads, n, c.head_dim)
+    for t in (k, v):
+        if t.dtype is not torch.bfloat16 or t.shape != shape or t.device != dev or t.stride(3) != 1:
+            raise ValueError("k and v must be bf16 tensors %s on %s, contiguous along their channels" % (list(shape), dev))
     ks, vs = k.stride(), v.stride()
     _call(lib().carnator_kv4_load, dev, ctypes.byref(c), _i32(table, "table", (B, W), dev), B, W,
           _i32(kv_len, "kv_len", (B,), dev), n, k.data_ptr(), ks[0], ks[1], ks[2], v.data_ptr(), vs[0], vs[1], vs[2])
@@ -795,24 +799,25 @@ def kv4_attn(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, q_start: 
     if out is None:
         out = torch.zeros(T, heads, c.head_dim, dtype=torch.bfloat16, device=dev)
     else:
-        _rows(out, "out", heads, c.head_dim, dev)
-        if out.shape[0] != T:
-            raise ValueError("out has %d rows, q %d" % (out.shape[0], T))
+        if not _is_rows(out, heads, c.head_dim, dev) or out.shape[0] != T:
+            raise ValueError("out must be a bf16 tensor [%d, %d, %d] on %s, contiguous along its channels"
+                             % (T, heads, c.head_dim, dev))
     if not return_lse:
         lse = None
     elif lse is None:
         lse = torch.zeros(T, heads, dtype=torch.float32, device=dev)
-    elif lse.dtype != torch.float32 or lse.device != dev or tuple(lse.shape) != (T, heads) or not lse.is_contiguous():
+    elif lse.dtype is not torch.float32 or lse.shape != (T, heads) or lse.device != dev or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [rows, heads] on the pool's device")
-    L = lib()
+    L, max_q, cr = lib(), int(max_q), ctypes.byref(c)
     if workspace is None:
-        need = L.carnator_kv4_attn_workspace_size(ctypes.byref(c), heads, T, B, W, int(max_q))
-        ws, size = (_workspace(need, dev), need) if need else (None, 0)
+        size = L.carnator_kv4_attn_workspace_size(cr, heads, T, B, W, max_q)
+        if size:
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
     else:
-        ws, size = workspace, workspace.numel()
-    _call(L.carnator_kv4_attn, dev, ctypes.byref(qr), T, heads, ctypes.byref(c), _i32(table, "table", (B, W), dev), B, W,
-          _i32(q_start, "q_start", (B + 1,), dev), _i32(kv_len, "kv_len", (B,), dev), int(max_q), int(bool(causal)),
-          float(scale), out.data_ptr(), out.stride(0), out.stride(1), _ptr(lse), _ptr(ws), size)
+        size = workspace.numel()
+    _call(L.carnator_kv4_attn, dev, ctypes.byref(qr), T, heads, cr, _i32(table, "table", (B, W), dev), B, W,
+          _i32(q_start, "q_start", (B + 1,), dev), _i32(kv_len, "kv_len", (B,), dev), max_q, 1 if causal else 0, scale,
+          out.data_ptr(), out.stride(0), out.stride(1), _ptr(lse), _ptr(workspace), size)
     return (out, lse) if return_lse else out
 
 

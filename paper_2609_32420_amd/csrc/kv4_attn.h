@@ -73,14 +73,19 @@ struct Cut {
   int over, upto;
   int tile_rows, tiles, chunk, chunks;
   int turns;  // of the grid of the kernel for many rows
+  int span;   // rows of a request and cached head that parts are kept for; 0: parts are kept by query row
   __device__ bool has(const Span &s) const { return s.rows > over && s.rows <= upto; }
 };
-// Results of the parts: outputs [n_rows * heads][chunks][d] not yet divided,
-// (reference, rounded sum, sum) beside them.
+// Results of the parts: outputs [..][chunks][d] not yet divided, (reference,
+// rounded sum, sum) beside them, by query row and head or, where that is less (a
+// padded batch, or one of few rows to a request), by request, cached head and row.
 struct Parts {
   float *o;
   float4 *ml;
 };
+__device__ inline int64_t part_of(const Kv4Attn &a, const Cut &cut, const Span &s, int b, int h, int row, int i, int hd) {
+  return (cut.span ? ((int64_t)b * a.c.heads + h) * cut.span + row : (int64_t)(s.q0 + i) * a.heads + hd) * cut.chunks;
+}
 
 // The kernel for many rows (kv4_tile_kernels.hip), without the joining; its last
 // few_groups workgroups take the batch's requests of few rows.

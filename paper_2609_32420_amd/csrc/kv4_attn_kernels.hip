@@ -28,14 +28,15 @@ join_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut many, Parts many_parts) {
   const int b = id % a.batch, i = id / a.batch;
   const Span sp = span_of(a, b);
   if (i * a.group >= sp.rows) return;
-  const bool is_few = few.has(sp);
-  const Cut &cut = is_few ? few : many;
-  const Parts &parts = is_few ? few_parts : many_parts;
+  // a single request is of many rows however few it has
+  const bool is_many = many.has(sp);
+  const Cut &cut = is_many ? many : few;
+  const Parts &parts = is_many ? many_parts : few_parts;
   const int row = i * a.group + hd % a.group;
   const int end = tile_end(a, sp, row - row % cut.tile_rows, cut.tile_rows);
   if (end <= cut.chunk) return;
   const int n = (end + cut.chunk - 1) / cut.chunk;
-  const int64_t at = ((int64_t)(sp.q0 + i) * a.heads + hd) * cut.chunks;
+  const int64_t at = part_of(a, cut, sp, b, hd / a.group, row, i, hd);
   float m = -INFINITY;
   for (int c = lane; c < n; c += 64) m = fmaxf(m, parts.ml[at + c].x);
 #pragma unroll
@@ -91,14 +92,14 @@ join_few_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut many, Parts many_parts,
   sp.rows = min(sp.m, a.max_q) * a.group;
   sp.kv = min(max(a.kv_len[b], 0), a.width << a.c.shift);
   if (i * a.group >= sp.rows) return;
-  const bool is_few = few.has(sp);
-  const Cut cut = is_few ? few : many;
-  const Parts parts = is_few ? few_parts : many_parts;
+  const bool is_many = many.has(sp);
+  const Cut cut = is_many ? many : few;
+  const Parts parts = is_many ? many_parts : few_parts;
   const int row = i * a.group + hd % a.group;
   const int end = tile_end(a, sp, row - row % cut.tile_rows, cut.tile_rows);
   if (end <= cut.chunk) return;
   const int n = (end + cut.chunk - 1) / cut.chunk;
-  const int64_t at = ((int64_t)(sp.q0 + i) * a.heads + hd) * cut.chunks;
+  const int64_t at = part_of(a, cut, sp, b, hd / a.group, row, i, hd);
   float m = -INFINITY;
   for (int c = 0; c < n; ++c) m = fmaxf(m, parts.ml[at + c].x);
   const float ref = m == -INFINITY ? 0.f : m;
@@ -151,6 +152,11 @@ void set_chunk(Cut &cut, int64_t reach, int64_t chunk) {
   cut.chunks = (int)up(reach, chunk);
 }
 
+// Keeps parts by request where that takes less than by query row.
+void set_span(const Kv4Attn &a, Cut &cut, int64_t rows) {
+  if (rows * a.batch * a.c.heads < (int64_t)a.n_rows * a.heads) cut.span = (int)rows;
+}
+
 // The requests of few rows.  One workgroup takes 0.7 us for its four waves' 128
 // tokens, and three of them fit a CU, so the axis is cut for about 640
 // workgroups; parts of 128 tokens to 1536 (longer ones balance ragged lengths
@@ -170,7 +176,8 @@ Cut few_cut(const Kv4Attn &a) {
   const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int64_t reach = (int64_t)a.width << a.c.shift;
   const int64_t base = (int64_t)a.batch * a.c.heads;
-  Cut cut{0, few_rows(a), 16 * nt, 1, (int)reach, 1, 1};
+  Cut cut{0, few_rows(a), 16 * nt, 1, (int)reach, 1, 1, 0};
+  set_span(a, cut, rows);
   if (reach <= 512 || (reach <= 1024 && base > 64)) return cut;
   const int64_t chunk = up(up(reach * base, 640), 128) * 128;
   set_chunk(cut, reach, chunk > 1536 ? 1536 : chunk);
@@ -191,8 +198,9 @@ Cut few_cut(const Kv4Attn &a) {
 //   444 tiles, 32,000: 863 / 1416 / 984 / 931
 Cut many_cut(const Kv4Attn &a) {
   const int64_t reach = (int64_t)a.width << a.c.shift;
-  Cut cut{few_rows(a), 0x7FFFFFFF, kTileRows, 0, (int)reach, 1, 0};
+  Cut cut{few_rows(a), 0x7FFFFFFF, kTileRows, 0, (int)reach, 1, 0, 0};
   if (most_rows(a) <= few_rows(a)) return cut;
+  set_span(a, cut, most_rows(a));
   if (a.batch == 1) cut.over = 0;  // a single request is left to this kernel however few rows it has
   cut.tiles = (int)up(most_rows(a), kTileRows);
   // tiles that hold rows, about: the requests' sum is at most n_rows
@@ -219,12 +227,13 @@ Cut many_cut(const Kv4Attn &a) {
 }
 
 // Scratch of a cut: the parts' outputs, then their references and sums.
-size_t outputs_bytes(const Kv4Attn &a, const Cut &cut) {
-  return align_up((size_t)a.n_rows * a.heads * cut.chunks * a.c.d * 4);
+size_t part_count(const Kv4Attn &a, const Cut &cut) {
+  return (cut.span ? (size_t)cut.span * a.batch * a.c.heads : (size_t)a.n_rows * a.heads) * cut.chunks;
 }
+size_t outputs_bytes(const Kv4Attn &a, const Cut &cut) { return align_up(part_count(a, cut) * a.c.d * 4); }
 size_t parts_bytes(const Kv4Attn &a, const Cut &cut) {
   if (cut.chunks == 1 || cut.tiles == 0) return 0;
-  return outputs_bytes(a, cut) + align_up((size_t)a.n_rows * a.heads * cut.chunks * 16);
+  return outputs_bytes(a, cut) + align_up(part_count(a, cut) * 16);
 }
 int64_t workgroups(const Kv4Attn &a, const Cut &cut) {
   return (int64_t)cut.turns * a.batch * a.c.heads * cut.chunks;

@@ -339,7 +339,7 @@ __device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a
     if (row >= sp.rows) continue;
     const int i = row / a.group, hd = h * a.group + row - i * a.group;
     if (SPLIT && !whole) {
-      const int64_t at = ((int64_t)(sp.q0 + i) * a.heads + hd) * cut.chunks + chunk;
+      const int64_t at = part_of(a, cut, sp, b, h, row, i, hd) + chunk;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll

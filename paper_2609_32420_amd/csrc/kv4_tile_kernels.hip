@@ -471,7 +471,7 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
   const float l = lh.x + lh.y;
   if (!live) return;
   if (!whole) {
-    const int64_t at = ((int64_t)(sp.q0 + qi) * a.heads + hd) * cut.chunks + chunk;
+    const int64_t at = part_of(a, cut, sp, b, h, row, qi, hd) + chunk;
 #pragma unroll
     for (int mo = 0; mo < D / 32; ++mo)
 #pragma unroll

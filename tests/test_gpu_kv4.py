@@ -222,9 +222,9 @@ def _check_attn(q, pool, table, q_start, kv_len, block, causal, scale=0.0, **kw)
     sigma = scale if scale > 0 else 1 / math.sqrt(d)
     out = torch.full_like(q, 7.0)
     lse = torch.full((T, heads), 7.0, device=DEV)
-    o, l = P.kv4_attn(q, pool, table, _i32(q_start), _i32(kv_len), kw.pop("max_q", max(1, max(
-        b - a for a, b in zip(q_start, q_start[1:])))), block, causal=causal, scale=scale, return_lse=True, out=out,
-        lse=lse, **kw)
+    most = kw.pop("max_q", None) or max(1, max(b - a for a, b in zip(q_start, q_start[1:])))
+    o, l = P.kv4_attn(q, pool, table, _i32(q_start), _i32(kv_len), most, block, causal=causal, scale=scale,
+                      return_lse=True, out=out, lse=lse, **kw)
     k, v = P.kv4_load(pool, table, _i32(kv_len), block)
     there = (table >= 0) & (table < pool.shape[0])
     done = torch.zeros(T, dtype=torch.bool, device=DEV)
@@ -255,8 +255,7 @@ def _check_attn(q, pool, table, q_start, kv_len, block, causal, scale=0.0, **kw)
             assert ((gl - ls).abs()[some] <= (off + n * 2.0 ** -23 + 2.0 ** -22 + ls.abs() * 2.0 ** -23)[some]).all()
     assert (o[~done] == 7).all() and (l[~done] == 7).all()
     # the same bits again, without the LSE, and in an output of the call's own
-    again = P.kv4_attn(q, pool, table, _i32(q_start), _i32(kv_len), max(1, max(b - a for a, b in zip(q_start, q_start[1:]))),
-                       block, causal=causal, scale=scale)
+    again = P.kv4_attn(q, pool, table, _i32(q_start), _i32(kv_len), most, block, causal=causal, scale=scale)
     assert torch.equal(again[done].view(torch.int16), o[done].view(torch.int16)) and (again[~done] == 0).all()
     return o, l
 
@@ -396,6 +395,34 @@ def test_attention_of_a_long_cache(m):
     pages = sum(-(-n // 128) for n in kv)
     pool = _filled(pages, 2, 128, 128, 4)
     _check_attn(_bf16(4 * m, 4, 128, seed=m), pool, _tables(kv, 128, pages, 3), [m * i for i in range(5)], kv, 128, True)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("most", [1, 9, 200])
+def test_attention_of_a_padded_batch(d, most):
+    # max_q far above the requests' rows, rows behind the last request, with a key axis that is cut
+    for kv, m in ([[5000], [1]], [[5000], [40]], [[5000, 900, 64], [1, 5, 3]], [[3000, 2000, 700], [150, 2, 1]]):
+        if max(m) > most:
+            continue
+        pages = sum(-(-n // 64) for n in kv)
+        pool = _filled(pages, 2, d, 64, 4)
+        start = [0] + np.cumsum(m).tolist()
+        _check_attn(_bf16(start[-1] + 700, 4, d, seed=most), pool, _tables(kv, 64, pages, 3), start, kv, 64, True, max_q=most)
+
+
+def test_rows_of_a_request_past_max_q_are_left_out():
+    pool, kv = _filled(9, 2, 64, 64, 4), [300, 200]
+    q, table = _bf16(150, 4, 64, seed=1), _tables(kv, 64, 9, 3)
+    # two kernels' answers, each off by at most (2^-8 + 2^-7 1.01) max |v| (see _check_attn)
+    bound = 0.025 * P.kv4_load(pool, table, _i32(kv), 64)[1].abs().max()
+    want = P.kv4_attn(q, pool, table, _i32([0, 140, 150]), _i32(kv), 140, 64, causal=True)
+    for most in (3, 10, 100):
+        out = torch.full_like(q, 7.0)
+        P.kv4_attn(q, pool, table, _i32([0, 140, 150]), _i32(kv), most, 64, causal=True, out=out)
+        for a, b in ((0, 140), (140, 150)):
+            end = min(b, a + most)
+            assert (out[a:end].float() - want[a:end].float()).abs().max() <= bound
+            assert (out[end:b] == 7).all()
 
 
 def test_a_workspace_is_used_up_to_its_size():

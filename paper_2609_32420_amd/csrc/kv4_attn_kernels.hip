@@ -140,10 +140,11 @@ int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
 // Rows of a request, at most.
 int64_t most_rows(const Kv4Attn &a) { return (int64_t)a.max_q * a.group; }
 
-// Rows of a request up to which rows_kernel takes it: at d = 128 the outputs of
-// 64 rows do not fit the registers of two waves a SIMD (8 heads, 16,000 tokens,
-// 48 rows: 35 us with one wave a SIMD, 23 in the other kernel).
-int few_rows(const Kv4Attn &a) { return a.c.d == 128 ? 32 : 64; }
+// Rows of a request up to which it is of few rows.  At d = 128 the outputs of 64
+// rows do not fit the registers of two waves a SIMD (8 heads, 16,000 tokens, 48
+// rows: 35 us with one wave a SIMD, 23 in the other kernel); at d = 64 they do, but
+// not those of the three that the other kernel runs with.
+int few_rows(const Kv4Attn &a) { return a.c.d == 64 && most_rows(a) <= 64 ? 64 : 32; }
 
 // Cuts the key axis into parts of `chunk` tokens (a multiple of 128).
 void set_chunk(Cut &cut, int64_t reach, int64_t chunk) {
@@ -187,11 +188,11 @@ Cut few_cut(const Kv4Attn &a) {
 // The requests of more rows (tiles is 0 where there can be none).  Parts of the
 // key axis fill CUs that the tiles leave empty and even out the last round, and
 // cost their outputs' way through memory; their number is the one with the least
-// time by this: a token of a tile takes 27 ns (19 at d = 64) with two workgroups
-// on the CU and 20 (14.6) with one, so 512 workgroups are a round
-// (half a one more than their number says, past two); a part of a
-// tile adds 0.03 us (half at d = 64) to the joining, which begins at 6 us.  Per call at d =
-// 128, whole / in parts of 512 / 2048 / 4096 tokens:
+// time by this.  A token of a tile takes 20, 27 ns with one or two workgroups on
+// the CU (d = 64: 14.6, 19, 28.6 with up to three).  Past two rounds half a one is
+// added, since workgroups do not end together.  A part of a tile adds 0.03 us (0.015)
+// to the joining, which begins at 6 us.  Per call at d = 128, whole / in parts of 512
+// / 2048 / 4096 tokens:
 //   8 tiles, 2000 tokens: 50 / 25 / - / - us (17 in parts of 128)
 //   60 tiles, 16,000: 317 / 109 / 86 / 103
 //   192 tiles, 16,000: 319 / 325 / 238 / 240
@@ -206,14 +207,17 @@ Cut many_cut(const Kv4Attn &a) {
   // tiles that hold rows, about: the requests' sum is at most n_rows
   const int64_t all = (int64_t)cut.tiles * a.batch, held = up((int64_t)a.n_rows * a.group, kTileRows);
   const int64_t base = (all < held ? all : held) * a.c.heads;
-  const double two = a.c.d == 128 ? 0.027 : 0.019, one = a.c.d == 128 ? 0.020 : 0.0146;
-  const double part = a.c.d == 128 ? 0.03 : 0.015;
+  const bool d128 = a.c.d == 128;
+  const int fit = d128 ? 2 : 3;  // workgroups on a CU
+  const double token[2][3] = {{0.0146, 0.019, 0.0286}, {0.020, 0.027, 0.027}};
+  const double part = d128 ? 0.03 : 0.015;
   double best = 1e300;
   for (int64_t n = 1; n <= kMaxParts && (n == 1 || reach >= n * 128); ++n) {
     const int64_t chunk = n == 1 ? reach : up(up(reach, n), 128) * 128;
-    const double rounds = base * n <= 256 ? one / two : base * n <= 1024 ? (double)up(base * n, 512)
-                                                                         : (double)(base * n) / 512 + 0.5;
-    const double us = rounds * two * (double)chunk + (n > 1 ? 6 + part * (double)(base * n) : 0);
+    const int64_t groups = base * n, round = 256 * fit;
+    const int64_t on_cu = up(groups, 256) < fit ? up(groups, 256) : fit;
+    const double rounds = groups <= 2 * round ? (double)up(groups, round) : (double)groups / round + 0.5;
+    const double us = rounds * token[d128][on_cu - 1] * (double)chunk + (n > 1 ? 6 + part * (double)groups : 0);
     if (us < best) {
       best = us;
       cut.chunk = (int)chunk;

@@ -58,7 +58,7 @@ struct TileCfg {
   static constexpr int RB = 2 * D;               // bytes of a K row
   static constexpr int TB = kKeys * RB;          // a converted tile of K or V
   static constexpr int POISON = 4 * TB;          // K slots 0, 1; V slots 0, 1; then token masks
-  static constexpr int NT = D == 128 ? 2 : 4;    // tiles of rows_body in the same workgroups
+  static constexpr int NT = 2;                   // tiles of rows_body in the same workgroups
   static constexpr int OWN = POISON + 2 * (D / 32) * 8;
   static constexpr int LDS = OWN > rows_lds(D, NT) ? OWN : rows_lds(D, NT);
   static_assert(UNITS >= 1, "a thread converts at least a unit");
@@ -66,7 +66,7 @@ struct TileCfg {
 };
 
 template <int D, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, 2)
+__global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2)
 tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
   using C = TileCfg<D, WAVES>;
   constexpr int UN = C::UNITS;
@@ -108,9 +108,9 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
   const int row = row0 + 32 * wave + l32;
   const int qi = row / a.group, hd = h * a.group + row - qi * a.group;
   const bool live = row < sp.rows;
-  const int limit = live ? sp.limit(a, qi) : sp.kv;
+  const int limit = min(live ? sp.limit(a, qi) : sp.kv, k_end);
   // tokens that every row of the wave sees
-  const int wave_all = row0 + 32 * wave < sp.rows ? sp.limit(a, (row0 + 32 * wave) / a.group) : sp.kv;
+  const int wave_all = min(row0 + 32 * wave < sp.rows ? sp.limit(a, (row0 + 32 * wave) / a.group) : sp.kv, k_end);
   bf16x8 qf[D / 16];
   {
     const uint16_t *qp = a.q.data + (int64_t)(sp.q0 + qi) * a.q.st + (int64_t)hd * a.q.sh + 8 * hh;
@@ -187,7 +187,11 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
     }
   };
   auto load_v = [&](Raw &x, const Stage &s) __attribute__((always_inline)) {
-    if (s.k >= k_end) return;
+    if (s.k >= k_end) {
+#pragma unroll
+      for (int i = 0; i < UN; ++i) x.w[i] = x.vs[i] = make_uint2(0, 0);
+      return;
+    }
     const unsigned char *base = a.c.pages + ((int64_t)s.page * a.c.heads + h) * rec;
     const int tp = s.k & (block - 1);
     const unsigned char *vb = base + codes + scales + tp * (D / 2), *vs = base + 2 * codes + scales + tp * (D / 32);
@@ -314,16 +318,13 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
   constexpr int PF = 4;               // operand reads run this many slots ahead
   constexpr int NPV = 4 * (D / 32);   // MFMAs of a P.V
   constexpr int NQK = 2 * (D / 16);   // MFMAs of a Q.K
-  using T = std::true_type;
-  using F = std::false_type;
 
-  // S, P and the walk
+  // S, P and the walk.  P(j) takes the place of P(j-1): its first half is formed
+  // when the products of the other's are done.
   f32x16 s[2];
-  u32x4 pa[4], pb[4];
+  u32x4 p[4];
   Soft st{-INFINITY, -INFINITY, 0.f, 0.f, 0.f};
-  auto iterate = [&](auto has_pv, auto odd, u32x4 (&pprev)[4], u32x4 (&pcur)[4], const Stage &sj, const Stage &s1,
-                     Raw &kraw, Raw &vraw, int k_prev) __attribute__((always_inline)) {
-    constexpr bool HP = decltype(has_pv)::value;
+  auto iterate = [&](auto odd, const Stage &sj, const Stage &s1, Raw &kraw, Raw &vraw, int k_prev) __attribute__((always_inline)) {
     constexpr int VS = decltype(odd)::value ? 0 : 1, KS = VS;  // slots of V(j-1) and K(j+1)
     constexpr int VW = 1 - VS, KW = 1 - KS;                   // of V(j) and K(j+2)
     st.m0 = st.m1 = -INFINITY;
@@ -334,28 +335,24 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
         vf[i] = *reinterpret_cast<const bf16x8 *>(lds + vread[i / (D / 32)] + VS * C::TB + (i % (D / 32)) * 32 * 128);
       };
       constexpr int NC = 8 + 1 + 8;  // maxima, alpha, exponentials of the first tile
-      if constexpr (HP) {
+      static_assert(9 * NPV / 17 >= NPV / 2, "P is formed where it has been used");
 #pragma unroll
-        for (int i = 0; i < PF; ++i) vrd(i);
-      }
+      for (int i = 0; i < PF; ++i) vrd(i);
 #pragma unroll
       for (int sl = 0; sl < NPV; ++sl) {
-        if constexpr (HP) {
-          if (sl + PF < NPV) vrd(sl + PF);
-          const int tp = sl / (D / 32), mo = sl % (D / 32);
-          o[mo] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[sl], __builtin_bit_cast(bf16x8, pprev[tp]), o[mo], 0, 0, 0);
-        }
+        if (sl + PF < NPV) vrd(sl + PF);
+        const int tp = sl / (D / 32), mo = sl % (D / 32);
+        o[mo] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[sl], __builtin_bit_cast(bf16x8, p[tp]), o[mo], 0, 0, 0);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           if (c * NPV / NC != sl) continue;
           if (c < 8) sm_max(st, s, 4 * c);
           else if (c < 9) sm_alpha(st);
-          else sm_exp(st, s, pcur, 2 * (c - 9));
+          else sm_exp(st, s, p, 2 * (c - 9));
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (HP)
-        if (k_prev + kKeys > seen_by_all) poison(k_prev, VS);
+      if (k_prev + kKeys > seen_by_all) poison(k_prev, VS);
     }
     {
       bf16x8 kf[NQK];
@@ -377,7 +374,7 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
 #pragma unroll
         for (int c = 0; c < NE; ++c) {
           if (c * HALF / NE != sl) continue;
-          if (c < 8) sm_exp(st, s, pcur, 16 + 2 * c);
+          if (c < 8) sm_exp(st, s, p, 16 + 2 * c);
           else sm_done(st);
         }
 #pragma unroll
@@ -414,6 +411,12 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
     put_all(1);
     load_k(kr, s2);
     load_v(vr, s0);
+    // stage -1: nothing, in the slot of odd stages
+#pragma unroll
+    for (int i = 0; i < C::TB / 16 / C::THREADS; ++i)
+      *reinterpret_cast<u32x4 *>(lds + 3 * C::TB + (threadIdx.x + i * C::THREADS) * 16) = u32x4{};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) p[t] = u32x4{};
     lds_barrier();
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
@@ -426,14 +429,13 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
       mask(s, 0, s0.k);
       mask(s, 1, s0.k);
     }
-    int k_prev = 0;
-    // iteration j: s0 = stage j, s1, s2 the next ones; kr, vr hold K(j+2), V(j)
-    auto turn = [&](auto first, auto odd) __attribute__((always_inline)) {
-      constexpr bool O = decltype(odd)::value;
+    int k_prev = -kKeys;
+    // iteration j: s0 = stage j, s1, s2 the next ones; kr, vr hold K(j+2), V(j).
+    // Iterations come in pairs; one past the last stage sees no token.
+    auto turn = [&](auto odd) __attribute__((always_inline)) {
       lds_barrier();
-      if constexpr (!decltype(first)::value) rescale();
-      iterate(std::integral_constant<bool, !decltype(first)::value>{}, odd, O ? pa : pb, O ? pb : pa, s0, s1, kr, vr,
-              k_prev);
+      rescale();
+      iterate(odd, s0, s1, kr, vr, k_prev);
       k_prev = s0.k;
       s0 = s1;
       s1 = s2;
@@ -441,29 +443,21 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
       load_k(kr, s2);
       load_v(vr, s0);
     };
-    turn(T{}, F{});
-    while (s1.k < k_end) {
-      turn(F{}, T{});
-      turn(F{}, F{});
-    }
-    const bool last_odd = s0.k < k_end;
-    if (last_odd) turn(F{}, T{});
-    // P.V of the last stage: V in slot 0 (P in pa) after an even one, else slot 1
-    auto finish_pv = [&](auto vs_c, const u32x4 (&p)[4]) __attribute__((always_inline)) {
-      constexpr int VS = decltype(vs_c)::value;
-      lds_barrier();
-      rescale();
+    do {
+      turn(std::false_type{});
+      turn(std::true_type{});
+    } while (s0.k < k_end);
+    // P.V of the last stage, an odd one
+    lds_barrier();
+    rescale();
 #pragma unroll
-      for (int tp = 0; tp < 4; ++tp)
+    for (int tp = 0; tp < 4; ++tp)
 #pragma unroll
-        for (int mo = 0; mo < D / 32; ++mo) {
-          const bf16x8 v = *reinterpret_cast<const bf16x8 *>(lds + vread[tp] + VS * C::TB + mo * 32 * 128);
-          o[mo] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, p[tp]), o[mo], 0, 0, 0);
-        }
-      if (k_prev + kKeys > seen_by_all) poison(k_prev, VS);
-    };
-    if (last_odd) finish_pv(std::integral_constant<int, 1>{}, pb);
-    else finish_pv(std::integral_constant<int, 0>{}, pa);
+      for (int mo = 0; mo < D / 32; ++mo) {
+        const bf16x8 v = *reinterpret_cast<const bf16x8 *>(lds + vread[tp] + C::TB + mo * 32 * 128);
+        o[mo] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, p[tp]), o[mo], 0, 0, 0);
+      }
+    if (k_prev + kKeys > seen_by_all) poison(k_prev, 1);
   }
 
   // ---- outputs: channels 32 mo + 8 g + 4 hh + i

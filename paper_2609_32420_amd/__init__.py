@@ -850,7 +850,7 @@ class Kv4Cache:
         q_start, kv_len, slots, positions, counts = page_plan(self.kv_len, new_len, self.table, self.free, self.block,
                                                               k.shape[0])
         kv4_store(self.pool, k, v, slots, self.block)
-        self.kv_len = kv_len
+        self.kv_len.copy_(kv_len)  # in place, as the table: a captured attention goes on reading it
         _, taken, lacking = counts.tolist()
         self.free = self.free[taken:]
         return q_start, positions, lacking

@@ -475,6 +475,30 @@ def test_another_stream_and_a_captured_graph():
             assert torch.equal(a, b)
 
 
+def test_a_captured_attention_sees_what_is_appended_after():
+    # decoding: attention captured once over the cache's own table and lengths,
+    # replayed between appends, a request emptied in between
+    block, heads, d = 64, 2, 64
+    cache = P.Kv4Cache(12, 2, 4, heads, d, block)
+    cache.append(_bf16(90, heads, d, seed=1), _bf16(90, heads, d, seed=2), _i32([62, 28]))
+    q, start = _bf16(2, 4, d, seed=3), _i32([0, 1, 2])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        held = cache.attn(q, start, 1, causal=True)
+    for i in range(5):
+        k, v = _bf16(2, heads, d, seed=10 + i), _bf16(2, heads, d, seed=20 + i)
+        assert cache.append(k, v, _i32([1, 1]))[2] == 0
+        if i == 3:
+            cache.release([1])
+        q.copy_(_bf16(2, 4, d, seed=30 + i))
+        want = cache.attn(q, start, 1, causal=True)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, want) and bool(want[1].any()) == (i < 3 or i == 4)
+
+
 # ---------------------------------------------------------------- together
 
 def test_a_cache_grows_token_by_token():

@@ -849,7 +849,12 @@ class Kv4Cache:
         entry in the table, which are not held."""
         q_start, kv_len, slots, positions, counts = page_plan(self.kv_len, new_len, self.table, self.free, self.block,
                                                               k.shape[0])
-        kv4_store(self.pool, k, v, slots, self.block)
+        try:
+            kv4_store(self.pool, k, v, slots, self.block)
+        except Exception:  # refused: the pages entered in the table are still free
+            held = (self.kv_len + (self.block - 1)) // self.block
+            self.table[torch.arange(self.table.shape[1], device=self.table.device) >= held[:, None]] = -1
+            raise
         self.kv_len.copy_(kv_len)  # in place, as the table: a captured attention goes on reading it
         _, taken, lacking = counts.tolist()
         self.free = self.free[taken:]

@@ -555,6 +555,22 @@ def test_a_cache_grows_token_by_token():
     assert lacking == max(0, 320 - 64 * free) and int(cache.kv_len[0]) == min(320, 64 * free)
 
 
+def test_a_refused_append_takes_no_pages():
+    block, heads, d = 64, 1, 64
+    cache = P.Kv4Cache(6, 2, 3, heads, d, block)
+    k = _bf16(70, heads, d, seed=1)
+    assert cache.append(k, k, _i32([70, 0]))[2] == 0
+    before = cache.table.clone(), cache.kv_len.clone(), cache.free.clone()
+    odd = _bf16(71 * d + 4)[4:].view(71, heads, d)  # 8 bytes off
+    for v, error in ((k.float(), ValueError), (k[:60], ValueError), (odd[:70], P.CarnatorError)):
+        with pytest.raises(error):
+            cache.append(k, v, _i32([60, 10]))
+        for got, want in zip((cache.table, cache.kv_len, cache.free), before):
+            assert torch.equal(got, want)
+    cache.release([0, 1])
+    assert sorted(cache.free.tolist()) == list(range(6))
+
+
 def test_context_of_a_region_from_the_cache():
     """A middle layer of a cache-hit request: keys and values of the context
     come from the history's cache, those of the active blocks are the target's

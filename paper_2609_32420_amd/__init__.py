@@ -657,6 +657,8 @@ def kv4_pool(n_pages: int, kv_heads: int, head_dim: int, block: int, device="cud
 def _kv4(pool: torch.Tensor, block: int) -> Kv4:
     if pool.dtype is not torch.uint8 or pool.dim() != 3 or not pool.is_cuda or not pool.is_contiguous():
         raise ValueError("pool must be a contiguous uint8 CUDA tensor [n_pages, kv_heads, block * d * 17 / 16]")
+    if block not in (64, 128):
+        raise ValueError("block must be 64 or 128 (got %r)" % (block,))
     n_pages, heads, size = pool.shape
     d = size * 16 // (17 * block)
     if block * d * 17 // 16 != size:

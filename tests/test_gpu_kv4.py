@@ -555,6 +555,16 @@ def test_a_cache_grows_token_by_token():
     assert lacking == max(0, 320 - 64 * free) and int(cache.kv_len[0]) == min(320, 64 * free)
 
 
+@pytest.mark.parametrize("block", [0, -64, 32, 96, 256])
+def test_binding_refuses_blocks_of_other_sizes(block):
+    pool, x = P.kv4_pool(3, 2, 64, 64), _bf16(4, 2, 64)
+    t, one = _i32([[0, 1]]), _i32([5])
+    for f in (lambda: P.kv4_store(pool, x, x, _i32([0] * 4), block), lambda: P.kv4_load(pool, t, one, block),
+              lambda: P.kv4_attn(x, pool, t, _i32([0, 4]), one, 4, block)):
+        with pytest.raises(ValueError):
+            f()
+
+
 def test_a_refused_append_takes_no_pages():
     block, heads, d = 64, 1, 64
     cache = P.Kv4Cache(6, 2, 3, heads, d, block)

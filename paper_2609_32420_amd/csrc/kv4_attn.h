@@ -89,7 +89,6 @@ __device__ inline int64_t part_of(const Kv4Attn &a, const Cut &cut, const Span &
 
 // The kernel for many rows (kv4_tile_kernels.hip), without the joining; its last
 // few_groups workgroups take the batch's requests of few rows.
-constexpr int kTileRows = 128;
 hipError_t launch_kv4_tiles(const Kv4Attn &a, const Cut &few, const Parts &few_parts, int few_groups, const Cut &cut,
                             const Parts &parts, hipStream_t s);
 

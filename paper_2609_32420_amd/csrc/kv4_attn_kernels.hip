@@ -10,7 +10,7 @@ template <int D, int NT, bool SPLIT>
 __global__ void __launch_bounds__(64 * kWaves, NT == 1 ? 3 : 2)
 rows_kernel(Kv4Attn a, Cut cut, Parts parts) {
   extern __shared__ float lds_rows[];
-  rows_body<D, NT, SPLIT>(a, cut, parts, (int)blockIdx.x, lds_rows);
+  rows_body<D, NT, SPLIT, kWaves>(a, cut, parts, (int)blockIdx.x, lds_rows);
 }
 
 // Joins the parts of a query row and head, in their order: a wave sums every
@@ -124,7 +124,7 @@ join_few_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut many, Parts many_parts,
 
 template <int D, int NT>
 hipError_t launch_rows(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s) {
-  const size_t lds = rows_lds(D, NT);
+  const size_t lds = rows_lds(D, NT, kWaves);
   const int64_t grid = (int64_t)cut.tiles * a.batch * a.c.heads * cut.chunks;
   const auto f = cut.chunks > 1 ? &rows_kernel<D, NT, true> : &rows_kernel<D, NT, false>;
   const hipError_t e = allow_lds(reinterpret_cast<const void *>(f), lds);
@@ -187,46 +187,61 @@ Cut few_cut(const Kv4Attn &a) {
 
 // The requests of more rows (tiles is 0 where there can be none).  Parts of the
 // key axis fill CUs that the tiles leave empty and even out the last round, and
-// cost their outputs' way through memory; their number is the one with the least
-// time by this.  A token of a tile takes 20, 27 ns with one or two workgroups on
-// the CU (d = 64: 14.6, 19, 28.6 with up to three).  Past two rounds half a one is
-// added, since workgroups do not end together.  A part of a tile adds 0.03 us (0.015)
-// to the joining, which begins at 6 us.  Per call at d = 128, whole / in parts of 512
-// / 2048 / 4096 tokens:
+// cost their outputs' way through memory.  At d = 128 a tile is 128 rows, two
+// workgroups to a CU, or 256, one of eight waves that convert a stage once where
+// two would do it twice: 12 heads of 4680 rows over 32,760 tokens 940 -> 840 us,
+// 40 of 1000 over 16,000 347 -> 319, but 12 requests of 24 heads, 798 rows and
+// 1427 tokens (a last tile nearly empty, start and end of a workgroup beside
+// nothing) 195 -> 241 and 8 of 400 over 2000 24.5 -> 28.1.  Taken are the tile
+// and the number of parts with the least time by this.  A token of a tile takes
+// 20, 27 ns with one or two workgroups on the CU (d = 64: 14.6, 19, 28.6 with up to
+// three), 24.6 and 4 us at the start with 256 rows.  Past two rounds half a one
+// is added, since workgroups do not end together.  A part of a tile adds 0.03 us
+// (0.015) to the joining, which begins at 6 us.  Over 70 calls drawn over the
+// whole range the choice is within 1 % of the better tile's time (geometric
+// mean; 15 % at worst).  Per call at d = 128, whole / in parts of 512 / 2048 / 4096
+// tokens, 128 rows:
 //   8 tiles, 2000 tokens: 50 / 25 / - / - us (17 in parts of 128)
 //   60 tiles, 16,000: 317 / 109 / 86 / 103
 //   192 tiles, 16,000: 319 / 325 / 238 / 240
 //   444 tiles, 32,000: 863 / 1416 / 984 / 931
+// Rows: d = 64; d = 128, 128 and 256 rows.  Columns: one, two, three workgroups on the CU.
+constexpr double kTokenUs[3][3] = {{0.0146, 0.019, 0.0286}, {0.020, 0.027, 0.027}, {0.0246, 0.0246, 0.0246}};
 Cut many_cut(const Kv4Attn &a) {
   const int64_t reach = (int64_t)a.width << a.c.shift;
-  Cut cut{few_rows(a), 0x7FFFFFFF, kTileRows, 0, (int)reach, 1, 0, 0};
+  Cut cut{few_rows(a), 0x7FFFFFFF, 128, 0, (int)reach, 1, 0, 0};
   if (most_rows(a) <= few_rows(a)) return cut;
   set_span(a, cut, most_rows(a));
   if (a.batch == 1) cut.over = 0;  // a single request is left to this kernel however few rows it has
-  cut.tiles = (int)up(most_rows(a), kTileRows);
-  // tiles that hold rows, about: the requests' sum is at most n_rows
-  const int64_t all = (int64_t)cut.tiles * a.batch, held = up((int64_t)a.n_rows * a.group, kTileRows);
-  const int64_t base = (all < held ? all : held) * a.c.heads;
   const bool d128 = a.c.d == 128;
-  const int fit = d128 ? 2 : 3;  // workgroups on a CU
-  const double token[2][3] = {{0.0146, 0.019, 0.0286}, {0.020, 0.027, 0.027}};
-  const double part = d128 ? 0.03 : 0.015;
   double best = 1e300;
-  for (int64_t n = 1; n <= kMaxParts && (n == 1 || reach >= n * 128); ++n) {
-    const int64_t chunk = n == 1 ? reach : up(up(reach, n), 128) * 128;
-    const int64_t groups = base * n, round = 256 * fit;
-    const int64_t on_cu = up(groups, 256) < fit ? up(groups, 256) : fit;
-    const double rounds = groups <= 2 * round ? (double)up(groups, round) : (double)groups / round + 0.5;
-    const double us = rounds * token[d128][on_cu - 1] * (double)chunk + (n > 1 ? 6 + part * (double)groups : 0);
-    if (us < best) {
-      best = us;
-      cut.chunk = (int)chunk;
-      cut.chunks = (int)up(reach, chunk);
+  for (int rows = 128; rows <= (d128 ? 256 : 128); rows *= 2) {
+    const int64_t tiles = up(most_rows(a), rows);
+    // tiles that hold rows, about: all of them where every request has max_q
+    // queries; else the requests' sum is n_rows, and the last tile half empty
+    const int64_t all = tiles * a.batch, held = up((int64_t)a.n_rows * a.group, rows) + a.batch / 2;
+    const int64_t base = ((int64_t)a.max_q * a.batch <= a.n_rows || all < held ? all : held) * a.c.heads;
+    const int fit = rows == 256 ? 1 : d128 ? 2 : 3;  // workgroups on a CU
+    const double *token = kTokenUs[rows == 256 ? 2 : d128];
+    const double start = rows == 256 ? 4 : 0, part = d128 ? 0.03 : 0.015;
+    for (int64_t n = 1; n <= kMaxParts && (n == 1 || reach >= n * 128); ++n) {
+      const int64_t chunk = n == 1 ? reach : up(up(reach, n), 128) * 128;
+      const int64_t groups = base * n, round = 256 * fit;
+      const int64_t on_cu = up(groups, 256) < fit ? up(groups, 256) : fit;
+      const double rounds = groups <= 2 * round ? (double)up(groups, round) : (double)groups / round + 0.5;
+      const double us = rounds * (token[on_cu - 1] * (double)chunk + start) + (n > 1 ? 6 + part * (double)groups : 0);
+      if (us < best) {
+        best = us;
+        cut.tile_rows = rows;
+        cut.tiles = (int)tiles;
+        cut.chunk = (int)chunk;
+        cut.chunks = (int)up(reach, chunk);
+      }
     }
   }
   cut.turns = cut.tiles;
   if (a.causal && a.batch > 1 && reach * a.group <= 4 * most_rows(a))
-    cut.turns += (int)(reach * a.group / kTileRows);
+    cut.turns += (int)(reach * a.group / cut.tile_rows);
   return cut;
 }
 

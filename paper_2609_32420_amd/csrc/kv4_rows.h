@@ -4,8 +4,7 @@
 //
 // A workgroup takes one request, one cached head and up to 16 NT query rows (a
 // row is a query token and one of the query heads that share the cached head,
-// so the cache is read once for all of them).  Its four waves take 32 tokens in
-// turn.  S = K Q^T and O^T += V^T P^T run on bf16 MFMA 16x16x32 with fp32
+// so the cache is read once for all of them).  Its waves take 32 tokens in turn.  S = K Q^T and O^T += V^T P^T run on bf16 MFMA 16x16x32 with fp32
 // accumulation, one pass with a running maximum and sum per query (fp32, exp2
 // domain).  Nothing passes through LDS: a lane's 16 bytes of K are one token's
 // 32 channels under one scale, which is its A operand once converted (the
@@ -14,17 +13,24 @@
 // are an A operand of V^T each once the two are told apart.  Rows of a K tile
 // are permuted so that the scores of eight consecutive tokens end in one lane,
 // as the B operand of the second product.
+//
+// Bound by the cache's bytes where there are many: 24 heads, d = 128, one query
+// over 119,056 tokens (389 MB) 75 us, 5.2 TB/s (the loads alone 71, the rest alone
+// 54); 47 requests of 32 / 8 heads and a query, 238,000 tokens in all (258 MB) 60
+// us.  A step's loads are issued one step ahead, and three waves fit a SIMD (two:
+// 112 us for the first, 86 with three before the axis was cut as now).  A short
+// cache is the latency of a launch and of one step: 12 heads, 77 tokens 4.7 us.
 #pragma once
 
 #include "kv4_attn.h"
 
 namespace carnator {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;  // of a workgroup of the kernel for few rows alone
 constexpr int kStep = 32;  // tokens of a wave's step
 
 // LDS of rows_body.
-constexpr int rows_lds(int d, int nt) { return 2 * nt * (d / 64 * 16 + 3) * 64 * 4; }
+constexpr int rows_lds(int d, int nt, int waves) { return waves / 2 * nt * (d / 64 * 16 + 3) * 64 * 4; }
 
 // What a wave reads of 32 tokens.
 template <int D>
@@ -36,12 +42,13 @@ struct Raw {
 };
 
 // Workgroup `id` of a grid of heads x tiles x batch x parts.
-template <int D, int NT, bool SPLIT>
-__device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a, const Cut &cut, const Parts &parts, int id, float *lds_o) {
+template <int D, int NT, bool SPLIT, int WAVES>
+__device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a, const Cut &cut, const Parts &parts, int id,
+                                                                float *lds_o) {
   constexpr int TQ = D / 32;        // products of a key tile
   constexpr int CPL = D / 4;        // channels of a lane
   constexpr int NV = D / 64;        // 64-channel parts of V
-  // lds_o: [2][NT * NV * 16][64] outputs, then [2][NT][3][64] references and sums
+  // lds_o: [WAVES / 2][NT * NV * 16][64] outputs, then [WAVES / 2][NT][3][64] references and sums
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, j = lane >> 4;
   const int h = id % a.c.heads;
@@ -105,7 +112,7 @@ __device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a
   int page = -1;
   // the first of the wave's steps from k0 on that has a page
   auto next = [&](int k0) {
-    for (; k0 < k_end; k0 += kWaves * kStep) {
+    for (; k0 < k_end; k0 += WAVES * kStep) {
       int at = (k0 >> a.c.shift) - entry0;
       if (at >= 64) {
         entry0 += at;
@@ -265,7 +272,7 @@ __device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a
   };
   // the loads of a step are under way during the one before
   Raw<D> even, odd;
-  const int stride = kWaves * kStep;
+  const int stride = WAVES * kStep;
   int k0 = next(k_first + wave * kStep);
   if (k0 < k_end) {
     load(even, k0);
@@ -288,7 +295,7 @@ __device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a
     lexact[n] += __shfl_xor(lexact[n], 16);
     lexact[n] += __shfl_xor(lexact[n], 32);
   }
-  float *ml = lds_o + 2 * NT * NV * 16 * 64;
+  float *ml = lds_o + WAVES / 2 * NT * NV * 16 * 64;
   auto put = [&](int slot) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -323,10 +330,13 @@ __device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a
             o[n][v][q][i] = o[n][v][q][i] * f1 + lds_o[((((slot * NT + n) * NV + v) * 4 + q) * 4 + i) * 64 + lane] * f2;
     }
   };
-  if (wave >= 2) put(wave - 2);
-  __syncthreads();
-  if (wave < 2) add(wave);
-  __syncthreads();
+#pragma unroll
+  for (int w = WAVES / 2; w > 1; w /= 2) {
+    if (wave >= w && wave < 2 * w) put(wave - w);
+    __syncthreads();
+    if (wave < w) add(wave);
+    __syncthreads();
+  }
   if (wave == 1) put(0);
   __syncthreads();
   if (wave != 0) return;

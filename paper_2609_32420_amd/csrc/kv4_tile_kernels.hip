@@ -16,6 +16,14 @@
 // += V(j-1)^T P(j-1)^T beside the maximum and half of the exponentials of S(j),
 // then S(j+1) beside the other half and beside the conversion of K(j+2) and
 // V(j), whose bytes were loaded during the iteration before.
+//
+// What bounds it is the issue of its instructions: beside an MFMA of 32 cycles a
+// wave issues 6.6 vector ones (d = 128), and MFMAs are under way 54 % of the time,
+// vector instructions 59 %, LDS 37 %.  12 heads, d = 128, 4680 queries over 32,760
+// tokens (942 GFLOP): 840-870 us with eight waves on a stage, 940-980 with four
+// (twice the conversions).  At d = 64 the softmax is twice as much beside an
+// MFMA, so three workgroups on a CU hide more of it than two: 1319 -> 1248 us for
+// 8 requests of 16 heads (4 cached) over 8192 tokens, 4096 queries each.
 #include "kv4_rows.h"
 
 #include <math.h>
@@ -60,9 +68,9 @@ struct TileCfg {
   static constexpr int POISON = 4 * TB;          // K slots 0, 1; V slots 0, 1; then token masks
   static constexpr int NT = 2;                   // tiles of rows_body in the same workgroups
   static constexpr int OWN = POISON + 2 * (D / 32) * 8;
-  static constexpr int LDS = OWN > rows_lds(D, NT) ? OWN : rows_lds(D, NT);
+  static constexpr int FEW = rows_lds(D, NT, WAVES);
+  static constexpr int LDS = OWN > FEW ? OWN : FEW;
   static_assert(UNITS >= 1, "a thread converts at least a unit");
-  static_assert(WAVES == kWaves, "rows_body runs in the same workgroups");
 };
 
 template <int D, int WAVES>
@@ -75,8 +83,7 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
   const int group = a.c.heads * a.batch * cut.chunks;
   const int turn_of = (int)blockIdx.x / group;
   if (turn_of >= cut.turns) {  // requests of few rows (a launch of their own would cost more than they)
-    rows_body<D, C::NT, true>(a, few, few_parts, (int)blockIdx.x - cut.turns * group,
-                                         reinterpret_cast<float *>(lds));
+    rows_body<D, C::NT, true, WAVES>(a, few, few_parts, (int)blockIdx.x - cut.turns * group, reinterpret_cast<float *>(lds));
     return;
   }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -504,8 +511,9 @@ hipError_t launch(const Kv4Attn &a, const Cut &few, const Parts &few_parts, int 
 
 hipError_t launch_kv4_tiles(const Kv4Attn &a, const Cut &few, const Parts &few_parts, int few_groups, const Cut &cut,
                             const Parts &parts, hipStream_t s) {
-  return a.c.d == 128 ? launch<128, 4>(a, few, few_parts, few_groups, cut, parts, s)
-                      : launch<64, 4>(a, few, few_parts, few_groups, cut, parts, s);
+  if (a.c.d == 64) return launch<64, 4>(a, few, few_parts, few_groups, cut, parts, s);
+  return cut.tile_rows == 256 ? launch<128, 8>(a, few, few_parts, few_groups, cut, parts, s)
+                              : launch<128, 4>(a, few, few_parts, few_groups, cut, parts, s);
 }
 
 }  // namespace carnator

@@ -398,6 +398,38 @@ def test_attention_of_a_long_cache(m):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("m,kv,kv_heads,group,causal", [
+    ([600, 3, 130], [2000, 300, 130], 44, 1, False), ([600, 3, 130], [1990, 300, 100], 22, 2, True),
+    ([900, 2, 30, 5], [4000, 1300, 64, 0], 1, 7, True), ([257, 255, 1], [2000, 64, 1], 48, 1, True)])
+def test_attention_that_fills_the_chip(d, m, kv, kv_heads, group, causal):
+    # tiles of 256 rows at d = 128, requests of few rows in the same grid, an axis in parts
+    pages = sum(-(-n // 64) for n in kv) + 1
+    pool = _filled(pages, kv_heads, d, 64, 6)
+    start = [0] + np.cumsum(m).tolist()
+    _check_attn(_bf16(start[-1] + 1, kv_heads * group, d, seed=d), pool, _tables(kv, 64, pages, 5), start, kv, 64, causal)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_that_are_masked_have_no_effect_where_tiles_fill_the_chip(d):
+    block, n, m, heads = 64, 2000, 260, 60
+    k, v = _bf16(n, heads, d, seed=1), _bf16(n, heads, d, seed=2)
+    slots = _i32(list(range(n)))
+    clean = P.kv4_pool(32, heads, d, block)
+    P.kv4_store(clean, k, v, slots, block)
+    pool = torch.full_like(clean, 255)  # behind the last token
+    v[n - 3, 1, 32], v[n - 150, 59, 5] = math.nan, math.inf
+    P.kv4_store(pool, k, v, slots, block)
+    q, args = _bf16(m, 2 * heads, d, seed=3), (_i32([list(range(32))]), _i32([0, m]), _i32([n]), m, block)
+    a = P.kv4_attn(q, clean, *args, causal=True, return_lse=True)
+    b = P.kv4_attn(q, pool, *args, causal=True, return_lse=True)
+    last = n - m + torch.arange(m, device=DEV)
+    nan = torch.zeros(m, 2 * heads, d, dtype=torch.bool, device=DEV)
+    nan[last >= n - 3, 2:4, 32:64] = True
+    nan[last >= n - 150, 118:, :32] = True
+    assert torch.equal(torch.isnan(b[0]), nan) and torch.equal(b[0][~nan], a[0][~nan]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("most", [1, 9, 200])
 def test_attention_of_a_padded_batch(d, most):
     # max_q far above the requests' rows, rows behind the last request, with a key axis that is cut

@@ -266,7 +266,8 @@ int carnator_select_block_mask(const double *mass, const carnator_shape *shape,
  * Cached keys and values held in 4 bits -- Sec. 3.3: tokens outside the
  * active region keep their cached computation.  Their K and V are kept in
  * pages of `block` tokens; a table names the pages of each request, so
- * requests share pages and a page can be left out.  The same calls serve a
+ * requests share pages (full ones: appending writes into a partly filled page,
+ * for every request that names it) and a page can be left out.  The same calls serve a
  * model that generates token by token or frame by frame: K and V of the new
  * tokens are appended, and their queries attend to what is cached.
  *

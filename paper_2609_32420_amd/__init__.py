@@ -828,7 +828,9 @@ class Kv4Cache:
     pages, the table and the length of each request, and the pages that are
     free, all on the device.  A page may be named by several requests' tables
     (a target that keeps the history's pages for the blocks it does not
-    recompute); a table entry of -1 leaves its block out."""
+    recompute); a table entry of -1 leaves its block out.  A request that
+    is appended to writes into its last page while that is partly filled, also
+    where another request names it: share full pages."""
 
     def __init__(self, n_pages: int, batch: int, width: int, kv_heads: int, head_dim: int, block: int, device="cuda"):
         self.block = block

@@ -18,12 +18,13 @@
 // V(j), whose bytes were loaded during the iteration before.
 //
 // What bounds it is the issue of its instructions: beside an MFMA of 32 cycles a
-// wave issues 6.6 vector ones (d = 128), and MFMAs are under way 54 % of the time,
-// vector instructions 59 %, LDS 37 %.  12 heads, d = 128, 4680 queries over 32,760
-// tokens (942 GFLOP): 840-870 us with eight waves on a stage, 940-980 with four
-// (twice the conversions).  At d = 64 the softmax is twice as much beside an
-// MFMA, so three workgroups on a CU hide more of it than two: 1319 -> 1248 us for
-// 8 requests of 16 heads (4 cached) over 8192 tokens, 4096 queries each.
+// wave issues 5.9 vector ones (d = 128; 12.7 at d = 64), and MFMAs are under way
+// 54 % (36) of the time, vector instructions 54 % (72), LDS 37 % (32).  12 heads, d =
+// 128, 4680 queries over 32,760 tokens (942 GFLOP): 840 to 895 us with eight waves
+// on a stage, 940 to 980 with four (twice the conversions).  At d = 64 the softmax
+// is twice as much beside an MFMA, so three workgroups on a CU hide more of it
+// than two: 1319 -> 1248 us for 8 requests of 16 heads (4 cached) over 8192 tokens,
+// 4096 queries each.
 #include "kv4_rows.h"
 
 #include <math.h>

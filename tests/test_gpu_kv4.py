@@ -531,6 +531,28 @@ def test_a_captured_attention_sees_what_is_appended_after():
         assert torch.equal(held, want) and bool(want[1].any()) == (i < 3 or i == 4)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_captured_call_of_many_rows(d):
+    # the largest tiles with requests of few rows beside them, joined parts; replayed with new queries
+    m, kv = [600, 3, 257], [2000, 300, 1500]
+    start = _i32([0] + np.cumsum(m).tolist())
+    for kv_heads, group in ((44, 1), (2, 3)):
+        pool, q = _filled(62, kv_heads, d, 64, 3), _bf16(860, kv_heads * group, d, seed=1)
+        args = (pool, _tables(kv, 64, 62, 2), start, _i32(kv), 600, 64)
+        P.kv4_attn(q, *args, causal=True)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            held = P.kv4_attn(q, *args, causal=True, return_lse=True)
+        for i in range(3):
+            q.copy_(_bf16(860, kv_heads * group, d, seed=10 + i))
+            want = P.kv4_attn(q, *args, causal=True, return_lse=True)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(held[0], want[0]) and torch.equal(held[1], want[1])
+
+
 # ---------------------------------------------------------------- together
 
 def test_a_cache_grows_token_by_token():

@@ -654,8 +654,11 @@ def kv4_pool(n_pages: int, kv_heads: int, head_dim: int, block: int, device="cud
     return torch.zeros(n_pages, kv_heads, block * head_dim * 17 // 16, dtype=torch.uint8, device=device)
 
 
+_UINT8, _INT32, _BF16 = torch.uint8, torch.int32, torch.bfloat16  # each look-up in torch costs a call 0.05 us
+
+
 def _kv4(pool: torch.Tensor, block: int) -> Kv4:
-    if pool.dtype is not torch.uint8 or pool.dim() != 3 or not pool.is_cuda or not pool.is_contiguous():
+    if pool.dtype is not _UINT8 or pool.dim() != 3 or not pool.is_cuda or not pool.is_contiguous():
         raise ValueError("pool must be a contiguous uint8 CUDA tensor [n_pages, kv_heads, block * d * 17 / 16]")
     if block not in (64, 128):
         raise ValueError("block must be 64 or 128 (got %r)" % (block,))
@@ -667,18 +670,18 @@ def _kv4(pool: torch.Tensor, block: int) -> Kv4:
 
 
 def _is_rows(t: torch.Tensor, heads: int, d: int, device) -> bool:
-    return (t.dtype is torch.bfloat16 and t.dim() == 3 and t.shape[1:] == (heads, d) and t.device == device
-            and t.stride(2) == 1)
+    if t.dtype is not _BF16 or t.dim() != 3 or t.device != device:
+        return False
+    _, h, c = t.shape
+    return h == heads and c == d and t.stride(2) == 1
 
 
 def _rows(t: torch.Tensor, name: str, heads: int, d: int, device) -> Rows:
     if not _is_rows(t, heads, d, device):
         raise ValueError("%s must be a bf16 tensor [rows, %d, %d] on %s, contiguous along its channels"
                          % (name, heads, d, device))
-    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
-
-
-_INT32 = torch.int32
+    st, sh, _ = t.stride()
+    return Rows(t.data_ptr(), st, sh)
 
 
 def _i32(t: torch.Tensor, name: str, shape, device) -> int:
@@ -721,15 +724,20 @@ def page_plan(kv_len: torch.Tensor, new_len: torch.Tensor, table: torch.Tensor, 
         if n_slots < 0:
             raise ValueError("n_slots must be >= 0")
         # one allocation for the five
-        out = torch.empty(2 * (B + n_slots) + 4, dtype=torch.int32, device=dev).split((n_slots, n_slots, B + 1, B, 3))
-        out = (out[2], out[3], out[0], out[1], out[4])
-    q_start, kv_out, slots, positions, counts = out
+        buf = torch.empty(2 * (B + n_slots) + 4, dtype=_INT32, device=dev)
+        slots, positions, q_start, kv_out, counts = buf.split((n_slots, n_slots, B + 1, B, 3))
+        at = buf.data_ptr()
+        to = (at + 8 * n_slots, at + 8 * n_slots + 4 * (B + 1), at, at + 4 * n_slots, at + 8 * n_slots + 8 * B + 4)
+    else:
+        q_start, kv_out, slots, positions, counts = out
+        to = (_i32(q_start, "q_start", (B + 1,), dev), _i32(kv_out, "kv_len_out", (B,), dev),
+              _i32(slots, "slots", (n_slots,), dev),
+              None if positions is None else _i32(positions, "positions", (n_slots,), dev),
+              _i32(counts, "counts", (3,), dev))
+    n_free = free_pages.shape[0]
     _call(lib().carnator_page_plan, dev, _i32(kv_len, "kv_len", (B,), dev), _i32(new_len, "new_len", (B,), dev), B,
-          _i32(table, "table", (B, W), dev), W, _i32(free_pages, "free_pages", (free_pages.shape[0],), dev),
-          free_pages.shape[0], int(block), _i32(q_start, "q_start", (B + 1,), dev),
-          _i32(kv_out, "kv_len_out", (B,), dev), _i32(slots, "slots", (n_slots,), dev),
-          None if positions is None else _i32(positions, "positions", (n_slots,), dev), n_slots,
-          _i32(counts, "counts", (3,), dev))
+          _i32(table, "table", (B, W), dev), W, _i32(free_pages, "free_pages", (n_free,), dev), n_free, int(block),
+          to[0], to[1], to[2], to[3], n_slots, to[4])
     return q_start, kv_out, slots, positions, counts
 
 
@@ -765,7 +773,7 @@ def kv4_load(pool: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, bloc
     n = k.shape[2] if n is None and k.dim() == 4 else n
     shape = (B, c.kv_heads, n, c.head_dim)
     for t in (k, v):
-        if t.dtype is not torch.bfloat16 or t.shape != shape or t.device != dev or t.stride(3) != 1:
+        if t.dtype is not _BF16 or t.shape != shape or t.device != dev or t.stride(3) != 1:
             raise ValueError("k and v must be bf16 tensors %s on %s, contiguous along their channels" % (list(shape), dev))
     ks, vs = k.stride(), v.stride()
     _call(lib().carnator_kv4_load, dev, ctypes.byref(c), _i32(table, "table", (B, W), dev), B, W,

@@ -14,6 +14,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMaxChunks = 256;
+constexpr int kShortJoin = 32;  // parts that join_kernel loads at once
 // Growth of the running maximum (log2 units) below which O and l keep their
 // scale: P may then reach 2^8, harmless in fp32 and bf16.
 constexpr float kSlack = 8.f;

@@ -878,7 +878,7 @@ class Kv4Cache:
         pages = self.table[requests].flatten()
         self.table[requests] = -1
         self.kv_len[requests] = 0
-        pages = pages[pages >= 0].unique()
+        pages = pages[(pages >= 0) & (pages < self.pool.shape[0])].unique()
         self.free = torch.cat([self.free, pages[~torch.isin(pages, self.table)]])
 
     def load(self, n: Optional[int] = None, out=None, keep=None):

@@ -635,6 +635,15 @@ def test_a_refused_append_takes_no_pages():
     assert sorted(cache.free.tolist()) == list(range(6))
 
 
+def test_entries_that_are_no_page_are_not_freed():
+    cache = P.Kv4Cache(5, 2, 4, 1, 64, 64)
+    k = _bf16(200, 1, 64, seed=1)
+    assert cache.append(k, k, _i32([190, 10]))[2] == 0
+    cache.table[0, 1:3] = _i32([5, 2 ** 30])  # outside the pool: their blocks are left out
+    cache.release([0])
+    assert sorted(cache.free.tolist()) == [0, 4]
+
+
 def test_context_of_a_region_from_the_cache():
     """A middle layer of a cache-hit request: keys and values of the context
     come from the history's cache, those of the active blocks are the target's

@@ -720,9 +720,9 @@ def page_plan(kv_len: torch.Tensor, new_len: torch.Tensor, table: torch.Tensor, 
         raise ValueError("expected kv_len [batch], table [batch, width] and free_pages [n]")
     B, W = kv_len.shape[0], table.shape[1]
     n_slots = int(n_slots)
+    if not 0 <= n_slots < 2 ** 31:
+        raise ValueError("n_slots must be 0 to 2^31 - 1")
     if out is None:
-        if n_slots < 0:
-            raise ValueError("n_slots must be >= 0")
         # one allocation for the five
         buf = torch.empty(2 * (B + n_slots) + 4, dtype=_INT32, device=dev)
         slots, positions, q_start, kv_out, counts = buf.split((n_slots, n_slots, B + 1, B, 3))
@@ -783,8 +783,9 @@ def kv4_load(pool: torch.Tensor, table: torch.Tensor, kv_len: torch.Tensor, bloc
 
 def kv4_attn_workspace(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, max_q: int, block: int) -> torch.Tensor:
     c = _kv4(pool, block)
-    return _workspace(lib().carnator_kv4_attn_workspace_size(ctypes.byref(c), q.shape[1], q.shape[0], table.shape[0],
-                                                             table.shape[1], int(max_q)), pool.device)
+    T = q.shape[0]
+    return _workspace(lib().carnator_kv4_attn_workspace_size(ctypes.byref(c), q.shape[1], T, table.shape[0],
+                                                             table.shape[1], min(int(max_q), max(T, 1))), pool.device)
 
 
 def kv4_attn(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
@@ -819,6 +820,8 @@ def kv4_attn(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, q_start: 
     elif lse.dtype is not torch.float32 or lse.shape != (T, heads) or lse.device != dev or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [rows, heads] on the pool's device")
     L, max_q, cr = lib(), int(max_q), ctypes.byref(c)
+    if max_q > T > 0:
+        max_q = T  # no request has more; a C int holds it
     if workspace is None:
         size = L.carnator_kv4_attn_workspace_size(cr, heads, T, B, W, max_q)
         if size:

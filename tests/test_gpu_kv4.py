@@ -635,6 +635,19 @@ def test_a_refused_append_takes_no_pages():
     assert sorted(cache.free.tolist()) == list(range(6))
 
 
+def test_sizes_that_a_c_int_does_not_hold():
+    pool, t, kv = _filled(4, 2, 64, 64, 1), _i32([[0, 2, 1]]), _i32([150])
+    q, start = _bf16(7, 4, 64, seed=2), _i32([0, 7])
+    want = P.kv4_attn(q, pool, t, start, kv, 7, 64, causal=True)
+    for most in (2 ** 31, 2 ** 32 + 1, 2 ** 63):
+        ws = P.kv4_attn_workspace(q, pool, t, most, 64)
+        assert torch.equal(P.kv4_attn(q, pool, t, start, kv, most, 64, causal=True), want)
+        assert torch.equal(P.kv4_attn(q, pool, t, start, kv, most, 64, causal=True, workspace=ws), want)
+    for n in (-1, 2 ** 31, 2 ** 32 + 8):
+        with pytest.raises(ValueError):
+            P.page_plan(kv, _i32([3]), t, _i32([3]), 64, n)
+
+
 def test_entries_that_are_no_page_are_not_freed():
     cache = P.Kv4Cache(5, 2, 4, 1, 64, 64)
     k = _bf16(200, 1, 64, seed=1)

@@ -52,15 +52,21 @@ struct Span {
     return a.causal ? min(max(kv - m + i + 1, 0), kv) : kv;
   }
 };
-__device__ inline Span span_of(const Kv4Attn &a, int b) {
-  const int q0 = __builtin_amdgcn_readfirstlane(a.q_start[b]), q1 = __builtin_amdgcn_readfirstlane(a.q_start[b + 1]);
-  const int kv = __builtin_amdgcn_readfirstlane(a.kv_len[b]);
+__device__ inline Span span_from(const Kv4Attn &a, int q0, int q1, int kv) {
   Span s;
   s.q0 = min(max(q0, 0), a.n_rows);
   s.m = min(max(q1, s.q0), a.n_rows) - s.q0;
   s.rows = min(s.m, a.max_q) * a.group;
   s.kv = min(max(kv, 0), a.width << a.c.shift);
   return s;
+}
+// Of a request that all lanes ask for, and of each lane's own.
+__device__ inline Span span_of(const Kv4Attn &a, int b) {
+  return span_from(a, __builtin_amdgcn_readfirstlane(a.q_start[b]), __builtin_amdgcn_readfirstlane(a.q_start[b + 1]),
+                   __builtin_amdgcn_readfirstlane(a.kv_len[b]));
+}
+__device__ inline Span lane_span_of(const Kv4Attn &a, int b) {
+  return span_from(a, a.q_start[b], a.q_start[b + 1], a.kv_len[b]);
 }
 // Tokens that the last of 16 NT rows from row0 on sees: what a tile walks.
 __device__ inline int tile_end(const Kv4Attn &a, const Span &s, int row0, int rows) {
@@ -73,10 +79,23 @@ __device__ inline int tile_end(const Kv4Attn &a, const Span &s, int row0, int ro
 struct Cut {
   int over, upto;
   int tile_rows, tiles, chunk, chunks;
-  int turns;  // of the grid of the kernel for many rows
+  int turns;  // of the kernel for many rows: a turn is a tile of every request
+  int items;  // tiles of its grid, each found in the turns by its number; 0: the grid holds the turns
   int span;   // rows of a request and cached head that parts are kept for; 0: parts are kept by query row
   __device__ bool has(const Span &s) const { return s.rows > over && s.rows <= upto; }
 };
+constexpr int kFindBatch = 1024;  // requests among which a tile is found by its number
+// Workgroups of a cut.
+inline int64_t tile_groups(const Kv4Attn &a, const Cut &cut) {
+  return (cut.items ? (int64_t)cut.items : (int64_t)cut.turns * a.batch) * a.c.heads * cut.chunks;
+}
+// Empty turns before a request's tiles: those of a request that ends `late` tiles'
+// tokens before the table does are that much later, so that a causal batch goes by
+// what its tiles see.
+template <int ROWS>
+__device__ inline int late_of(const Kv4Attn &a, const Cut &cut, const Span &s) {
+  return cut.turns > cut.tiles ? (int)((int64_t)((a.width << a.c.shift) - s.kv) * a.group / ROWS) : 0;
+}
 // Results of the parts: outputs [..][chunks][d] not yet divided, (reference,
 // rounded sum, sum) beside them, by query row and head or, where that is less (a
 // padded batch, or one of few rows to a request), by request, cached head and row.
@@ -88,8 +107,8 @@ __device__ inline int64_t part_of(const Kv4Attn &a, const Cut &cut, const Span &
   return (cut.span ? ((int64_t)b * a.c.heads + h) * cut.span + row : (int64_t)(s.q0 + i) * a.heads + hd) * cut.chunks;
 }
 
-// The kernel for many rows (kv4_tile_kernels.hip), without the joining; its last
-// few_groups workgroups take the batch's requests of few rows.
+// The kernel for many rows (kv4_tile_kernels.hip), without the joining; its first or
+// last few_groups workgroups take the batch's requests of few rows.
 hipError_t launch_kv4_tiles(const Kv4Attn &a, const Cut &few, const Parts &few_parts, int few_groups, const Cut &cut,
                             const Parts &parts, hipStream_t s);
 

@@ -13,21 +13,38 @@ rows_kernel(Kv4Attn a, Cut cut, Parts parts) {
   rows_body<D, NT, SPLIT, kWaves>(a, cut, parts, (int)blockIdx.x, lds_rows);
 }
 
+// Query i of request b, by its number: most to a request (most > 0), or by its row
+// (a ragged batch has far fewer of these).
+struct Query {
+  int b, i;  // b < 0: of no request
+};
+__device__ inline Query query_of(const Kv4Attn &a, int64_t id, int most) {
+  if (most) return Query{(int)(id / most) < a.batch ? (int)(id / most) : -1, (int)(id % most)};
+  int b = 0, end = a.batch;
+  if (id >= a.n_rows || id < a.q_start[0] || id >= a.q_start[end]) return Query{-1, 0};
+  while (end - b > 1) {  // q_start[b] <= id < q_start[end]
+    const int mid = (b + end) >> 1;
+    if (a.q_start[mid] <= id) b = mid;
+    else end = mid;
+  }
+  return Query{b, (int)id - max(a.q_start[b], 0)};
+}
+
 // Joins the parts of a query row and head, in their order: a wave sums every
 // fourth part, 64 lanes over the channels.  SHORT: 32 parts at most, whose loads are
 // all under way while the factors are formed (16 requests, 64 heads on 8 cached
 // ones over 3000 tokens 19.5 -> 18.7 us a call; with 78 parts it costs 1 us instead).
 template <int D, bool SHORT>
 __global__ void __launch_bounds__(64 * kWaves)
-join_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut many, Parts many_parts) {
+join_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut many, Parts many_parts, int most) {
   constexpr int C = D / 64;  // channels of a lane
   __shared__ float factor[SHORT ? 1 : kMaxChunks];
   __shared__ float sums[kWaves][D];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int id = (int)blockIdx.x;
-  const int hd = id % a.heads;
-  id /= a.heads;
-  const int b = id % a.batch, i = id / a.batch;
+  const int hd = (int)blockIdx.x % a.heads;
+  const Query query = query_of(a, (int)blockIdx.x / a.heads, most);
+  const int b = __builtin_amdgcn_readfirstlane(query.b), i = __builtin_amdgcn_readfirstlane(query.i);
+  if (b < 0) return;
   const Span sp = span_of(a, b);
   if (i * a.group >= sp.rows) return;
   // a single request is of many rows however few it has
@@ -111,14 +128,10 @@ join_few_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut many, Parts many_parts,
   int64_t id = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   const int c4 = 4 * (threadIdx.x % LANES);
   const int hd = (int)(id % a.heads);
-  id /= a.heads;
-  const int i = (int)(id % most), b = (int)(id / most);
-  if (b >= a.batch) return;
-  Span sp;  // of this lane's request (a workgroup may hold rows of two)
-  sp.q0 = min(max(a.q_start[b], 0), a.n_rows);
-  sp.m = min(max(a.q_start[b + 1], sp.q0), a.n_rows) - sp.q0;
-  sp.rows = min(sp.m, a.max_q) * a.group;
-  sp.kv = min(max(a.kv_len[b], 0), a.width << a.c.shift);
+  const Query query = query_of(a, id / a.heads, most);
+  const int b = query.b, i = query.i;
+  if (b < 0) return;
+  const Span sp = lane_span_of(a, b);  // a workgroup may hold rows of two requests
   if (i * a.group >= sp.rows) return;
   const bool is_many = many.has(sp);
   const Cut cut = is_many ? many : few;
@@ -217,14 +230,20 @@ void set_span(const Kv4Attn &a, Cut &cut, int64_t rows) {
 //   192 heads, 4096: 39.5 / 30.2 / 26.8 / 25.4 / 27.8 / 30.3
 //   128 heads, 16,384: 121 / 85 / 69 / 57 / 60 / 120
 // The lengths are on the device: the table's width is what the axis may reach.
-Cut few_cut(const Kv4Attn &a) {
+// Beside requests of many rows that keep the chip for at least twice as long
+// as a whole axis takes (many_us, 0 without them, or where they are joined anyway)
+// it stays whole too: a prompt of 2000 beside 60 single tokens, 32 / 8 heads, d = 128,
+// 4000 cached 113 -> 103 us.
+Cut few_cut(const Kv4Attn &a, double many_us) {
   const int64_t rows = most_rows(a) < few_rows(a) ? most_rows(a) : few_rows(a);
   const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int64_t reach = (int64_t)a.width << a.c.shift;
   const int64_t base = (int64_t)a.batch * a.c.heads;
-  Cut cut{0, few_rows(a), 16 * nt, 1, (int)reach, 1, 1, 0};
+  Cut cut{0, few_rows(a), 16 * nt, 1, (int)reach, 1, 1, 0, 0};
   set_span(a, cut, rows);
-  if (reach <= 512 || (reach <= 1024 && base > 64)) return cut;
+  if (reach <= 512 || (reach <= 1024 && base > 64) ||
+      (reach <= 8192 && 2 * 0.7 / 128 * (double)reach <= many_us))
+    return cut;
   const int64_t chunk = up(up(reach * base, 640), 128) * 128;
   set_chunk(cut, reach, chunk > 1536 ? 1536 : chunk);
   return cut;
@@ -250,22 +269,35 @@ Cut few_cut(const Kv4Attn &a) {
 //   60 tiles, 16,000: 317 / 109 / 86 / 103
 //   192 tiles, 16,000: 319 / 325 / 238 / 240
 //   444 tiles, 32,000: 863 / 1416 / 984 / 931
+// A ragged batch has tiles of all lengths, the longest first: it takes as long as
+// the longest (the requests of most rows see seven tenths of the table, say) or as
+// the work, half of the table for each, on all slots.  Tiles of 256 rows leave the
+// requests of few rows in the same grid two thirds of the waves, so they are for
+// batches of mostly long requests.  5 prompts, 9622 queries, 16 / 4 heads, d = 128:
+// 174 us with 256 rows, 196 with 128; one of 4096 beside 30 of a token and 8000 cached
+// 149 in three parts of 256 rows, 103 whole with 128.
 // Rows: d = 64; d = 128, 128 and 256 rows.  Columns: one, two, three workgroups on the CU.
 constexpr double kTokenUs[3][3] = {{0.0146, 0.019, 0.0286}, {0.020, 0.027, 0.027}, {0.0246, 0.0246, 0.0246}};
-Cut many_cut(const Kv4Attn &a) {
+Cut many_cut(const Kv4Attn &a, double *whole_us) {
+  *whole_us = 0;
   const int64_t reach = (int64_t)a.width << a.c.shift;
-  Cut cut{few_rows(a), 0x7FFFFFFF, 128, 0, (int)reach, 1, 0, 0};
+  Cut cut{few_rows(a), 0x7FFFFFFF, 128, 0, (int)reach, 1, 0, 0, 0};
   if (most_rows(a) <= few_rows(a)) return cut;
   set_span(a, cut, most_rows(a));
   if (a.batch == 1) cut.over = 0;  // a single request is left to this kernel however few rows it has
   const bool d128 = a.c.d == 128;
+  const bool ragged = (int64_t)a.max_q * a.batch > a.n_rows;
+  const int64_t long_ones = a.n_rows / a.max_q;
+  const bool large = d128 && (!ragged || a.batch <= 4 * long_ones);
   double best = 1e300;
-  for (int rows = 128; rows <= (d128 ? 256 : 128); rows *= 2) {
+  for (int rows = 128; rows <= (large ? 256 : 128); rows *= 2) {
     const int64_t tiles = up(most_rows(a), rows);
     // tiles that hold rows, about: all of them where every request has max_q
-    // queries; else the requests' sum is n_rows, and the last tile half empty
-    const int64_t all = tiles * a.batch, held = up((int64_t)a.n_rows * a.group, rows) + a.batch / 2;
-    const int64_t base = ((int64_t)a.max_q * a.batch <= a.n_rows || all < held ? all : held) * a.c.heads;
+    // queries; else the requests' sum is n_rows, and the last tiles half empty of
+    // twice as many requests as could be that long
+    const int64_t halves = a.batch / 2 < long_ones ? a.batch / 2 : long_ones;
+    const int64_t all = tiles * a.batch, held = up((int64_t)a.n_rows * a.group, rows) + halves;
+    const int64_t base = (!ragged || all < held ? all : held) * a.c.heads;
     const int fit = rows == 256 ? 1 : d128 ? 2 : 3;  // workgroups on a CU
     const double *token = kTokenUs[rows == 256 ? 2 : d128];
     const double start = rows == 256 ? 4 : 0, part = d128 ? 0.03 : 0.015;
@@ -274,7 +306,11 @@ Cut many_cut(const Kv4Attn &a) {
       const int64_t groups = base * n, round = 256 * fit;
       const int64_t on_cu = up(groups, 256) < fit ? up(groups, 256) : fit;
       const double rounds = groups <= 2 * round ? (double)up(groups, round) : (double)groups / round + 0.5;
-      const double us = rounds * (token[on_cu - 1] * (double)chunk + start) + (n > 1 ? 6 + part * (double)groups : 0);
+      const double work = ragged ? (double)base * 0.5 * (double)reach * token[fit - 1] / (double)round : 0;
+      const double seen = 0.7 * (double)reach < (double)chunk ? 0.7 * (double)reach : (double)chunk;
+      const double longest = 0.5 * (token[0] + token[fit - 1]) * seen + start;
+      const double us = (!ragged ? rounds * (token[on_cu - 1] * (double)chunk + start) : longest > work ? longest : work) +
+                        (n > 1 ? 6 + part * (double)groups : 0);
       if (us < best) {
         best = us;
         cut.tile_rows = rows;
@@ -284,10 +320,29 @@ Cut many_cut(const Kv4Attn &a) {
       }
     }
   }
+  if (cut.chunks == 1 && cut.over > 0) *whole_us = best;
   cut.turns = cut.tiles;
   if (a.causal && a.batch > 1 && reach * a.group <= 4 * most_rows(a))
     cut.turns += (int)(reach * a.group / cut.tile_rows);
+  // Ragged batches: the turns hold many tiles that there are not, each a workgroup
+  // that starts to find nothing; the rows leave at most `most` (a part of a tile a
+  // request, of those with more than `over` rows).  Finding a tile by its number
+  // takes a workgroup half a microsecond.  A prompt of 4096 beside 30 single tokens,
+  // 16 / 4 heads, 8000 cached: d = 64 117 -> 75 us, d = 128 (with the choices above)
+  // 424 -> 103.
+  const int64_t rows = (int64_t)a.n_rows * a.group, some = rows / (cut.over + 1);
+  const int64_t most = rows / cut.tile_rows + (some < a.batch ? some : a.batch);
+  if (a.batch > 1 && a.batch <= kFindBatch && 2 * (int64_t)cut.turns * a.batch > 3 * most) cut.items = (int)(most ? most : 1);
   return cut;
+}
+
+struct Cuts {
+  Cut few, many;
+};
+Cuts cuts(const Kv4Attn &a) {
+  double whole_us;
+  const Cut many = many_cut(a, &whole_us);
+  return Cuts{few_cut(a, whole_us), many};
 }
 
 // Scratch of a cut: the parts' outputs, then their references and sums.
@@ -299,23 +354,29 @@ size_t parts_bytes(const Kv4Attn &a, const Cut &cut) {
   if (cut.chunks == 1 || cut.tiles == 0) return 0;
   return outputs_bytes(a, cut) + align_up(part_count(a, cut) * 16);
 }
-int64_t workgroups(const Kv4Attn &a, const Cut &cut) {
-  return (int64_t)cut.turns * a.batch * a.c.heads * cut.chunks;
-}
-// Query rows of a request that a second kernel joins.
-int joined_rows(const Kv4Attn &a, const Cut &few, const Cut &many) {
-  if (many.tiles > 0 && many.chunks > 1) return a.max_q;
-  if (many.over == 0 || few.chunks == 1) return 0;
-  return few.upto < most_rows(a) ? few.upto / a.group : a.max_q;
+// Queries that a second kernel looks at, and of them `most` to a request (0: by row).
+struct Joined {
+  int64_t queries;
+  int most;
+};
+Joined joined(const Kv4Attn &a, const Cut &few, const Cut &many) {
+  int most = a.max_q;
+  if (!(many.tiles > 0 && many.chunks > 1)) {
+    if (many.over == 0 || few.chunks == 1) return Joined{0, 0};
+    if (few.upto < most_rows(a)) most = few.upto / a.group;
+  }
+  const int64_t all = (int64_t)most * a.batch;
+  return 2 * all > 3 * (int64_t)a.n_rows ? Joined{a.n_rows, 0} : Joined{all, most};
 }
 Parts parts_at(const Kv4Attn &a, const Cut &cut, char *at) {
   return Parts{reinterpret_cast<float *>(at), reinterpret_cast<float4 *>(at + outputs_bytes(a, cut))};
 }
 
 hipError_t launch_join(const Kv4Attn &a, const Cut &few, const Parts &fp, const Cut &many, const Parts &mp, hipStream_t s) {
-  const int most = joined_rows(a, few, many);
-  if (most == 0) return hipSuccess;
-  const int64_t n = (int64_t)most * a.batch * a.heads;
+  const Joined join = joined(a, few, many);
+  if (join.queries == 0) return hipSuccess;
+  const int64_t n = join.queries * a.heads;
+  const int most = join.most;
   const bool d128 = a.c.d == 128;
   const int parts = many.tiles > 0 && many.chunks > 1 ? many.chunks : few.chunks;
   if (parts <= 16 && n >= 2048) {
@@ -326,7 +387,7 @@ hipError_t launch_join(const Kv4Attn &a, const Cut &few, const Parts &fp, const 
     const bool is_short = (many.tiles > 0 && many.chunks > few.chunks ? many.chunks : few.chunks) <= kShortJoin;
     const auto f = d128 ? (is_short ? &join_kernel<128, true> : &join_kernel<128, false>)
                         : (is_short ? &join_kernel<64, true> : &join_kernel<64, false>);
-    hipLaunchKernelGGL(f, dim3((unsigned)n), dim3(64 * kWaves), 0, s, a, few, fp, many, mp);
+    hipLaunchKernelGGL(f, dim3((unsigned)n), dim3(64 * kWaves), 0, s, a, few, fp, many, mp, most);
   }
   return hipGetLastError();
 }
@@ -334,22 +395,25 @@ hipError_t launch_join(const Kv4Attn &a, const Cut &few, const Parts &fp, const 
 }  // namespace
 
 int64_t kv4_attn_workgroups(const Kv4Attn &a) {
-  const Cut few = few_cut(a), many = many_cut(a);
-  const int64_t main = workgroups(a, few) + workgroups(a, many);
-  const int64_t join = (int64_t)joined_rows(a, few, many) * a.batch * a.heads;
+  const auto [few, many] = cuts(a);
+  const int64_t main = tile_groups(a, few) + tile_groups(a, many);
+  const int64_t join = joined(a, few, many).queries * a.heads;
   return main > join ? main : join;
 }
 
-size_t kv4_attn_scratch_bytes(const Kv4Attn &a) { return parts_bytes(a, few_cut(a)) + parts_bytes(a, many_cut(a)); }
+size_t kv4_attn_scratch_bytes(const Kv4Attn &a) {
+  const auto [few, many] = cuts(a);
+  return parts_bytes(a, few) + parts_bytes(a, many);
+}
 
 hipError_t launch_kv4_attn(const Kv4Attn &a, void *scratch, hipStream_t s) {
-  const Cut few = few_cut(a), many = many_cut(a);
+  const auto [few, many] = cuts(a);
   char *at = static_cast<char *>(scratch);
   const Parts fp = parts_at(a, few, at), mp = parts_at(a, many, at + parts_bytes(a, few));
   hipError_t e;
   const bool d128 = a.c.d == 128;
   if (many.tiles > 0)
-    e = launch_kv4_tiles(a, few, fp, many.over == 0 ? 0 : (int)workgroups(a, few), many, mp, s);
+    e = launch_kv4_tiles(a, few, fp, many.over == 0 ? 0 : (int)tile_groups(a, few), many, mp, s);
   else if (few.tile_rows == 16)
     e = d128 ? launch_rows<128, 1>(a, few, fp, s) : launch_rows<64, 1>(a, few, fp, s);
   else if (few.tile_rows == 32)

@@ -74,17 +74,80 @@ struct TileCfg {
   static_assert(UNITS >= 1, "a thread converts at least a unit");
 };
 
+// Sum over a wave's lanes, in every lane.
+__device__ inline int wave_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);  // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+// Turn and request of tile `item` in the order of the turns, where a request has
+// `late` empty ones before its tiles; request -1 behind the last tile.  A lane
+// holds the requests lane + 64 k, k < K.
+template <int ROWS, int K>
+__device__ inline int2 find_tile(const Kv4Attn &a, const Cut &cut, int item) {
+  const int lane = threadIdx.x & 63;
+  int n[K], late[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    n[k] = late[k] = 0;
+    const int b = lane + 64 * k;
+    if (64 * k < a.batch && b < a.batch) {
+      const Span sp = lane_span_of(a, b);
+      if (cut.has(sp)) n[k] = (sp.rows + ROWS - 1) / ROWS;
+      late[k] = late_of<ROWS>(a, cut, sp);
+    }
+  }
+  const auto before = [&](int t) {  // tiles of the turns before t
+    int s = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (64 * k < a.batch) s += min(max(t - late[k], 0), n[k]);
+    return wave_sum(s);
+  };
+  int t = 0, end = cut.turns, first = 0;
+  if (item >= before(end)) return make_int2(0, -1);
+  while (end - t > 1) {  // before(t) <= item < before(end)
+    const int mid = (t + end) >> 1, s = before(mid);
+    if (s <= item) {
+      t = mid;
+      first = s;
+    } else {
+      end = mid;
+    }
+  }
+  int left = item - first, b = -1;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (64 * k >= a.batch) break;
+    const uint64_t in = __ballot(t >= late[k] && t - late[k] < n[k]);
+    const int count = __builtin_popcountll(in);
+    if (b < 0 && left < count) {
+      const int rank = __builtin_amdgcn_mbcnt_hi((unsigned)(in >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in, 0));
+      b = 64 * k + __builtin_ctzll(__ballot((in >> lane & 1) && rank == left));
+    }
+    left -= count;
+  }
+  return make_int2(t, b);
+}
+
 template <int D, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 3 : 2)
-tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
+tile_kernel(Kv4Attn a, Cut few, Parts few_parts, int few_first, Cut cut, Parts parts) {
   using C = TileCfg<D, WAVES>;
   constexpr int UN = C::UNITS;
   constexpr int ROWS = 32 * WAVES;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-  const int group = a.c.heads * a.batch * cut.chunks;
-  const int turn_of = (int)blockIdx.x / group;
-  if (turn_of >= cut.turns) {  // requests of few rows (a launch of their own would cost more than they)
-    rows_body<D, C::NT, true, WAVES>(a, few, few_parts, (int)blockIdx.x - cut.turns * group, reinterpret_cast<float *>(lds));
+  const int group = a.c.heads * cut.chunks * (cut.items ? 1 : a.batch), groups = cut.items ? cut.items : cut.turns;
+  const int place = (int)blockIdx.x - few_first;
+  int turn_of = place / group;
+  if (place < 0 || turn_of >= groups) {  // requests of few rows (a launch of their own would cost more than they)
+    const int id = place < 0 ? (int)blockIdx.x : place - groups * group;
+    rows_body<D, C::NT, true, WAVES>(a, few, few_parts, id, reinterpret_cast<float *>(lds));
     return;
   }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -93,15 +156,22 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut cut, Parts parts) {
   // the heads, requests and parts of a tile are rotated from tile to tile where
   // their number is even: otherwise the long ones of a ragged batch, or the early
   // parts of a causal one, would all meet on a few XCDs.
-  int id = (int)blockIdx.x - turn_of * group;
+  int id = place - turn_of * group;
   if (group % 2 == 0) id = (id + turn_of) % group;
   const int h = id % a.c.heads;
   id /= a.c.heads;
-  const int b = id % a.batch, chunk = id / a.batch;
+  int b, chunk = id;
+  if (cut.items) {
+    const int2 found = a.batch <= 64 ? find_tile<ROWS, 1>(a, cut, turn_of) : find_tile<ROWS, kFindBatch / 64>(a, cut, turn_of);
+    turn_of = found.x;
+    b = found.y;
+    if (b < 0) return;
+  } else {
+    b = id % a.batch;
+    chunk = id / a.batch;
+  }
   const Span sp = span_of(a, b);
-  // a causal batch by what the tiles see: the tiles of a request that ends
-  // `late` tiles' tokens before the table does are that much later
-  const int late = cut.turns > cut.tiles ? (int)((int64_t)((a.width << a.c.shift) - sp.kv) * a.group / ROWS) : 0;
+  const int late = late_of<ROWS>(a, cut, sp);
   const int tile = (sp.rows + ROWS - 1) / ROWS - 1 - (turn_of - late);
   const int row0 = tile * ROWS;
   if (!cut.has(sp) || turn_of < late || tile < 0) return;
@@ -503,8 +573,11 @@ hipError_t launch(const Kv4Attn &a, const Cut &few, const Parts &few_parts, int 
   using C = TileCfg<D, WAVES>;
   const hipError_t e = allow_lds(reinterpret_cast<const void *>(&tile_kernel<D, WAVES>), C::LDS);
   if (e != hipSuccess) return e;
-  const int64_t grid = (int64_t)cut.turns * a.batch * a.c.heads * cut.chunks + few_groups;
-  hipLaunchKernelGGL((tile_kernel<D, WAVES>), dim3((unsigned)grid), dim3(C::THREADS), C::LDS, s, a, few, few_parts, cut, parts);
+  const int64_t grid = tile_groups(a, cut) + few_groups;
+  // what is not cut begins first, what is cut fills the end
+  const int few_first = few.chunks == 1 ? few_groups : 0;
+  hipLaunchKernelGGL((tile_kernel<D, WAVES>), dim3((unsigned)grid), dim3(C::THREADS), C::LDS, s, a, few, few_parts,
+                     few_first, cut, parts);
   return hipGetLastError();
 }
 

@@ -410,6 +410,22 @@ def test_attention_that_fills_the_chip(d, m, kv, kv_heads, group, causal):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("batch", [2, 63, 64, 65, 200, 700, 1025])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_of_a_ragged_batch(d, batch, causal):
+    # one long prompt among short ones, single tokens and requests without queries
+    rng = np.random.default_rng(batch)
+    m = np.where(rng.random(batch) < 0.3, rng.integers(33, 180, batch), rng.integers(0, 3, batch))
+    m[batch // 2] = 900
+    kv = np.where(rng.random(batch) < 0.2, 0, m + rng.integers(0, 200, batch))
+    kv[0] = 1100
+    pages = sum(-(-int(n) // 64) for n in kv)
+    pool = _filled(pages, 1, d, 64, 6)
+    start = [0] + np.cumsum(m).tolist()
+    _check_attn(_bf16(start[-1] + 1, 2, d, seed=d), pool, _tables(kv.tolist(), 64, pages, 5), start, kv.tolist(), 64, causal)
+
+
+@pytest.mark.parametrize("d", [64, 128])
 def test_values_that_are_masked_have_no_effect_where_tiles_fill_the_chip(d):
     block, n, m, heads = 64, 2000, 260, 60
     k, v = _bf16(n, heads, d, seed=1), _bf16(n, heads, d, seed=2)

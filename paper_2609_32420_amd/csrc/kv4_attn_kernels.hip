@@ -180,10 +180,13 @@ join_few_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut many, Parts many_parts,
   if (a.lse && c4 == 0) a.lse[(int64_t)(sp.q0 + i) * a.heads + hd] = lse_of(m, le);
 }
 
+// Workgroups for the requests of few rows.
+int64_t few_groups(const Kv4Attn &a, const Cut &cut) { return (int64_t)a.batch * a.c.heads * cut.columns; }
+
 template <int D, int NT>
 hipError_t launch_rows(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s) {
   const size_t lds = rows_lds(D, NT, kWaves);
-  const int64_t grid = (int64_t)cut.tiles * a.batch * a.c.heads * cut.chunks;
+  const int64_t grid = few_groups(a, cut);
   const auto f = cut.chunks > 1 ? &rows_kernel<D, NT, true> : &rows_kernel<D, NT, false>;
   const hipError_t e = allow_lds(reinterpret_cast<const void *>(f), lds);
   if (e != hipSuccess) return e;
@@ -192,6 +195,7 @@ hipError_t launch_rows(const Kv4Attn &a, const Cut &cut, const Parts &parts, hip
 }
 
 constexpr int kMaxParts = 64;  // parts of the requests of many rows
+constexpr int kFewGroups = 8192;  // workgroups for the requests of few rows
 
 int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
 
@@ -234,18 +238,24 @@ void set_span(const Kv4Attn &a, Cut &cut, int64_t rows) {
 // as a whole axis takes (many_us, 0 without them, or where they are joined anyway)
 // it stays whole too: a prompt of 2000 beside 60 single tokens, 32 / 8 heads, d = 128,
 // 4000 cached 113 -> 103 us.
+// A table may be far wider than what is cached: of more than 8192 workgroups, some
+// thousand of which start to find nothing in a microsecond, the grid holds the
+// first parts, and a workgroup goes on to later ones.  48 requests of 1000 tokens,
+// 32 / 8 heads, d = 128, a table for 131,072: 43.6 us without, 18.6 so.
 Cut few_cut(const Kv4Attn &a, double many_us) {
   const int64_t rows = most_rows(a) < few_rows(a) ? most_rows(a) : few_rows(a);
   const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int64_t reach = (int64_t)a.width << a.c.shift;
   const int64_t base = (int64_t)a.batch * a.c.heads;
-  Cut cut{0, few_rows(a), 16 * nt, 1, (int)reach, 1, 1, 0, 0};
+  Cut cut{0, few_rows(a), 16 * nt, 1, (int)reach, 1, 1, 0, 1, 0};
   set_span(a, cut, rows);
   if (reach <= 512 || (reach <= 1024 && base > 64) ||
       (reach <= 8192 && 2 * 0.7 / 128 * (double)reach <= many_us))
     return cut;
   const int64_t chunk = up(up(reach * base, 640), 128) * 128;
   set_chunk(cut, reach, chunk > 1536 ? 1536 : chunk);
+  const int64_t columns = kFewGroups / base > 1 ? kFewGroups / base : 1;
+  cut.columns = (int)(cut.chunks < columns ? cut.chunks : columns);
   return cut;
 }
 
@@ -281,7 +291,7 @@ constexpr double kTokenUs[3][3] = {{0.0146, 0.019, 0.0286}, {0.020, 0.027, 0.027
 Cut many_cut(const Kv4Attn &a, double *whole_us) {
   *whole_us = 0;
   const int64_t reach = (int64_t)a.width << a.c.shift;
-  Cut cut{few_rows(a), 0x7FFFFFFF, 128, 0, (int)reach, 1, 0, 0, 0};
+  Cut cut{few_rows(a), 0x7FFFFFFF, 128, 0, (int)reach, 1, 0, 0, 0, 0};
   if (most_rows(a) <= few_rows(a)) return cut;
   set_span(a, cut, most_rows(a));
   if (a.batch == 1) cut.over = 0;  // a single request is left to this kernel however few rows it has
@@ -328,7 +338,7 @@ Cut many_cut(const Kv4Attn &a, double *whole_us) {
   // that starts to find nothing; the rows leave at most `most` (a part of a tile a
   // request, of those with more than `over` rows).  Finding a tile by its number
   // takes a workgroup half a microsecond.  A prompt of 4096 beside 30 single tokens,
-  // 16 / 4 heads, 8000 cached: d = 64 117 -> 75 us, d = 128 (with the choices above)
+  // 16 / 4 heads, 8000 cached: d = 64 117 -> 94 us, d = 128 (with the choices above)
   // 424 -> 103.
   const int64_t rows = (int64_t)a.n_rows * a.group, some = rows / (cut.over + 1);
   const int64_t most = rows / cut.tile_rows + (some < a.batch ? some : a.batch);
@@ -396,7 +406,7 @@ hipError_t launch_join(const Kv4Attn &a, const Cut &few, const Parts &fp, const 
 
 int64_t kv4_attn_workgroups(const Kv4Attn &a) {
   const auto [few, many] = cuts(a);
-  const int64_t main = tile_groups(a, few) + tile_groups(a, many);
+  const int64_t main = few_groups(a, few) + tile_groups(a, many);
   const int64_t join = joined(a, few, many).queries * a.heads;
   return main > join ? main : join;
 }
@@ -413,7 +423,7 @@ hipError_t launch_kv4_attn(const Kv4Attn &a, void *scratch, hipStream_t s) {
   hipError_t e;
   const bool d128 = a.c.d == 128;
   if (many.tiles > 0)
-    e = launch_kv4_tiles(a, few, fp, many.over == 0 ? 0 : (int)tile_groups(a, few), many, mp, s);
+    e = launch_kv4_tiles(a, few, fp, many.over == 0 ? 0 : (int)few_groups(a, few), many, mp, s);
   else if (few.tile_rows == 16)
     e = d128 ? launch_rows<128, 1>(a, few, fp, s) : launch_rows<64, 1>(a, few, fp, s);
   else if (few.tile_rows == 32)

@@ -41,27 +41,21 @@ struct Raw {
   uint2 vs[D / 64];  // the octet's scales
 };
 
-// Workgroup `id` of a grid of heads x tiles x batch x parts.
+// Part `chunk` (0 unless SPLIT) of request b, cached head h.
 template <int D, int NT, bool SPLIT, int WAVES>
-__device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a, const Cut &cut, const Parts &parts, int id,
-                                                                float *lds_o) {
+__device__ __attribute__((always_inline)) inline void rows_part(const Kv4Attn &a, const Cut &cut, const Parts &parts, const Span &sp,
+                                                                int b, int h, int chunk, float *lds_o) {
   constexpr int TQ = D / 32;        // products of a key tile
   constexpr int CPL = D / 4;        // channels of a lane
   constexpr int NV = D / 64;        // 64-channel parts of V
   // lds_o: [WAVES / 2][NT * NV * 16][64] outputs, then [WAVES / 2][NT][3][64] references and sums
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int tid = threadIdx.x;
+  if constexpr (SPLIT) asm volatile("" : "+v"(tid));  // what follows from it is not kept over rows_body's loop
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, j = lane >> 4;
-  const int h = id % a.c.heads;
-  id /= a.c.heads;
-  const int tile = id % cut.tiles;
-  id /= cut.tiles;
-  const int b = id % a.batch, chunk = SPLIT ? id / a.batch : 0;
-  const Span sp = span_of(a, b);
-  const int row0 = tile * 16 * NT;
-  if (!cut.has(sp) || row0 >= sp.rows) return;
+  constexpr int row0 = 0;
   const int end = tile_end(a, sp, row0, 16 * NT);  // tokens that a row of the tile sees
   const int k_first = SPLIT ? chunk * cut.chunk : 0;
-  if (k_first >= end && chunk > 0) return;
   const bool whole = !SPLIT || end <= cut.chunk;  // nothing to join
   const int k_end = SPLIT ? min(end, k_first + cut.chunk) : end;
   const int seen_by_all = sp.limit(a, row0 / a.group);
@@ -371,6 +365,30 @@ __device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a
         *reinterpret_cast<bf16x8 *>(op + 64 * v + 8 * half) = w;
       }
     if (a.lse && j == 0) a.lse[(int64_t)(sp.q0 + i) * a.heads + hd] = lse_of(mrun[n], lexact[n]);
+  }
+}
+
+// Workgroup `id` of a grid of heads x batch x columns.
+template <int D, int NT, bool SPLIT, int WAVES>
+__device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a, const Cut &cut, const Parts &parts, int id,
+                                                                float *lds_o) {
+  const int h = id % a.c.heads;
+  id /= a.c.heads;
+  const int b = id % a.batch;
+  const Span sp = span_of(a, b);
+  if (!cut.has(sp)) return;
+  if constexpr (!SPLIT) {
+    rows_part<D, NT, false, WAVES>(a, cut, parts, sp, b, h, 0, lds_o);
+  } else {
+    const int end = tile_end(a, sp, 0, 16 * NT);
+    int chunk = id / a.batch;
+    if (chunk > 0 && chunk * cut.chunk >= end) return;
+    for (;;) {
+      rows_part<D, NT, true, WAVES>(a, cut, parts, sp, b, h, chunk, lds_o);
+      chunk += cut.columns;
+      if (chunk >= cut.chunks || chunk * cut.chunk >= end) return;
+      __syncthreads();  // LDS is free again
+    }
   }
 }
 

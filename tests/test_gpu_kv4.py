@@ -426,6 +426,21 @@ def test_attention_of_a_ragged_batch(d, batch, causal):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("most", [1, 40])
+def test_attention_with_a_table_far_wider_than_the_lengths(d, most):
+    # a workgroup takes several parts of a long request in turn
+    batch, kv_heads = 36, 120
+    m = [1 + b % 3 * (most > 1) for b in range(batch)]
+    kv = [1 + 5 * b for b in range(batch)]
+    m[20], m[7], kv[20], kv[3] = most, 0, 5000, 3100
+    pages = sum(-(-n // 64) for n in kv)
+    pool = _filled(pages, kv_heads, d, 64, 6)
+    start = [0] + np.cumsum(m).tolist()
+    table = _tables(kv, 64, pages, 5, width=600)
+    _check_attn(_bf16(start[-1], kv_heads, d, seed=d), pool, table, start, kv, 64, True)
+
+
+@pytest.mark.parametrize("d", [64, 128])
 def test_values_that_are_masked_have_no_effect_where_tiles_fill_the_chip(d):
     block, n, m, heads = 64, 2000, 260, 60
     k, v = _bf16(n, heads, d, seed=1), _bf16(n, heads, d, seed=2)

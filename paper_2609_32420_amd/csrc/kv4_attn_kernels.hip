@@ -280,12 +280,14 @@ Cut few_cut(const Kv4Attn &a, double many_us) {
 //   192 tiles, 16,000: 319 / 325 / 238 / 240
 //   444 tiles, 32,000: 863 / 1416 / 984 / 931
 // A ragged batch has tiles of all lengths, the longest first: it takes as long as
-// the longest (the requests of most rows see seven tenths of the table, say) or as
-// the work, half of the table for each, on all slots.  Tiles of 256 rows leave the
+// the longest (the requests of most rows see two thirds of the table, say) or as
+// the work, three tenths of the table for each, on all slots (parts cost 1.3 times
+// as much there); over 40 such calls drawn over the whole range that is within 4 %
+// of the best cut (geometric mean; 23 % at worst).  Tiles of 256 rows leave the
 // requests of few rows in the same grid two thirds of the waves, so they are for
 // batches of mostly long requests.  5 prompts, 9622 queries, 16 / 4 heads, d = 128:
 // 174 us with 256 rows, 196 with 128; one of 4096 beside 30 of a token and 8000 cached
-// 149 in three parts of 256 rows, 103 whole with 128.
+// 149 in three parts of 256 rows, 106 whole with 128.
 // Rows: d = 64; d = 128, 128 and 256 rows.  Columns: one, two, three workgroups on the CU.
 constexpr double kTokenUs[3][3] = {{0.0146, 0.019, 0.0286}, {0.020, 0.027, 0.027}, {0.0246, 0.0246, 0.0246}};
 Cut many_cut(const Kv4Attn &a, double *whole_us) {
@@ -310,14 +312,14 @@ Cut many_cut(const Kv4Attn &a, double *whole_us) {
     const int64_t base = (!ragged || all < held ? all : held) * a.c.heads;
     const int fit = rows == 256 ? 1 : d128 ? 2 : 3;  // workgroups on a CU
     const double *token = kTokenUs[rows == 256 ? 2 : d128];
-    const double start = rows == 256 ? 4 : 0, part = d128 ? 0.03 : 0.015;
+    const double start = rows != 256 ? 0 : ragged ? 8 : 4, part = (d128 ? 0.03 : 0.015) * (ragged ? 1.3 : 1);
     for (int64_t n = 1; n <= kMaxParts && (n == 1 || reach >= n * 128); ++n) {
       const int64_t chunk = n == 1 ? reach : up(up(reach, n), 128) * 128;
       const int64_t groups = base * n, round = 256 * fit;
       const int64_t on_cu = up(groups, 256) < fit ? up(groups, 256) : fit;
       const double rounds = groups <= 2 * round ? (double)up(groups, round) : (double)groups / round + 0.5;
-      const double work = ragged ? (double)base * 0.5 * (double)reach * token[fit - 1] / (double)round : 0;
-      const double seen = 0.7 * (double)reach < (double)chunk ? 0.7 * (double)reach : (double)chunk;
+      const double work = ragged ? (double)base * 0.3 * (double)reach * token[fit - 1] / (double)round : 0;
+      const double seen = 0.65 * (double)reach < (double)chunk ? 0.65 * (double)reach : (double)chunk;
       const double longest = 0.5 * (token[0] + token[fit - 1]) * seen + start;
       const double us = (!ragged ? rounds * (token[on_cu - 1] * (double)chunk + start) : longest > work ? longest : work) +
                         (n > 1 ? 6 + part * (double)groups : 0);

@@ -510,10 +510,7 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, int few_first, Cut cut, Parts p
     int k_prev = -kKeys;
     // iteration j: s0 = stage j, s1, s2 the next ones; kr, vr hold K(j+2), V(j).
     // Iterations come in pairs; one past the last stage sees no token.
-    auto turn = [&](auto odd) __attribute__((always_inline)) {
-      lds_barrier();
-      rescale();
-      iterate(odd, s0, s1, kr, vr, k_prev);
+    auto advance = [&]() __attribute__((always_inline)) {
       k_prev = s0.k;
       s0 = s1;
       s1 = s2;
@@ -521,6 +518,34 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, int few_first, Cut cut, Parts p
       load_k(kr, s2);
       load_v(vr, s0);
     };
+    auto turn = [&](auto odd) __attribute__((always_inline)) {
+      lds_barrier();
+      rescale();
+      iterate(odd, s0, s1, kr, vr, k_prev);
+      advance();
+    };
+    if (row0 + 32 * wave >= sp.rows) {
+      // a wave without rows (the last tile of a request) converts its share
+      int slot = 0;
+      do {
+        lds_barrier();
+        if (s0.k + kKeys > seen_by_all) clean_v(vr, s0.k, slot);
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+          uint32_t tv[8];
+          put_k(kr, i, 0, slot);
+          put_k(kr, i, 1, slot);
+          conv_v(vr, i, 0, tv);
+          conv_v(vr, i, 1, tv);
+          put_v(tv, i, 0, slot);
+          put_v(tv, i, 1, slot);
+        }
+        advance();
+        slot ^= 1;
+      } while (s0.k < k_end || slot == 1);
+      lds_barrier();
+      return;
+    }
     do {
       turn(std::false_type{});
       turn(std::true_type{});

@@ -2,17 +2,17 @@
 // active region keep their cached computation), for each request's queries over
 // the pages that its table names.
 //
-// A workgroup takes one request, one cached head and up to 16 NT query rows (a
-// row is a query token and one of the query heads that share the cached head,
-// so the cache is read once for all of them).  Its waves take 32 tokens in turn.  S = K Q^T and O^T += V^T P^T run on bf16 MFMA 16x16x32 with fp32
-// accumulation, one pass with a running maximum and sum per query (fp32, exp2
-// domain).  Nothing passes through LDS: a lane's 16 bytes of K are one token's
-// 32 channels under one scale, which is its A operand once converted (the
-// channels are dealt to the four products in the same order for Q), and a
-// lane's bytes of V are the eight tokens of an octet for two channels, which
-// are an A operand of V^T each once the two are told apart.  Rows of a K tile
-// are permuted so that the scores of eight consecutive tokens end in one lane,
-// as the B operand of the second product.
+// A workgroup takes one request, one cached head and up to 16 NT query rows (a row
+// is a query token and one of the query heads that share the cached head, so the
+// cache is read once for all of them). Its waves take 32 tokens in turn. S = K Q^T
+// and O^T += V^T P^T run on bf16 MFMA 16x16x32 with fp32 accumulation, one pass
+// with a running maximum and sum per query (fp32, exp2 domain). Nothing passes
+// through LDS: a lane's 16 bytes of K are one token's 32 channels under one scale,
+// which is its A operand once converted (the channels are dealt to the four
+// products in the same order for Q), and a lane's bytes of V are the eight tokens
+// of an octet for two channels, which are an A operand of V^T each once the two
+// are told apart. Rows of a K tile are permuted so that the scores of eight
+// consecutive tokens end in one lane, as the B operand of the second product.
 //
 // Bound by the cache's bytes where there are many: 24 heads, d = 128, one query
 // over 119,056 tokens (389 MB) 75 us, 5.2 TB/s (the loads alone 71, the rest alone
@@ -43,8 +43,8 @@ struct Raw {
 
 // Part `chunk` (0 unless SPLIT) of request b, cached head h.
 template <int D, int NT, bool SPLIT, int WAVES>
-__device__ __attribute__((always_inline)) inline void rows_part(const Kv4Attn &a, const Cut &cut, const Parts &parts, const Span &sp,
-                                                                int b, int h, int chunk, float *lds_o) {
+__device__ __attribute__((always_inline)) inline void rows_part(const Kv4Attn &a, const Cut &cut, const Parts &parts,
+                                                                const Span &sp, int b, int h, int chunk, float *lds_o) {
   constexpr int TQ = D / 32;        // products of a key tile
   constexpr int CPL = D / 4;        // channels of a lane
   constexpr int NV = D / 64;        // 64-channel parts of V

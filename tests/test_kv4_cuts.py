@@ -1,0 +1,85 @@
+"""How attention over 4-bit cached keys and values is cut into workgroups: the
+host's choice (no GPU) for the sizes that the GPU tests below run."""
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+import paper_2609_32420_amd as P
+from paper_2609_32420_amd import build as B
+from test_gpu_kv4 import _bf16, _check_attn, _filled, _tables
+
+CSRC = os.path.join(os.path.dirname(P.__file__), "csrc")
+INCLUDE = os.path.join(B.ROOT, "include")
+
+PROBE = r"""
+#include "kv4_cut.h"
+#include <stdio.h>
+using namespace carnator;
+int main() {
+  long long d, kv_heads, heads, rows, batch, width, block, max_q, causal;
+  while (scanf("%lld %lld %lld %lld %lld %lld %lld %lld %lld", &d, &kv_heads, &heads, &rows, &batch, &width, &block,
+               &max_q, &causal) == 9) {
+    Kv4Attn a{};
+    a.c = Kv4{nullptr, 1 << 20, (int)kv_heads, (int)d, block == 64 ? 6 : 7};
+    a.heads = (int)heads, a.group = (int)(heads / kv_heads), a.n_rows = (int)rows, a.batch = (int)batch;
+    a.width = (int)width, a.max_q = (int)(max_q < rows ? max_q : rows), a.causal = (int)causal;
+    const auto [few, many] = cuts(a);
+    printf("tile_rows %d few_chunks %d many_tiles %d many_chunks %d turns %d items %d bytes %zu groups %lld\n",
+           many.tile_rows, few.chunks, many.tiles, many.chunks, many.turns, many.items,
+           parts_bytes(a, few) + parts_bytes(a, many), (long long)(few_groups(a, few) + tile_groups(a, many)));
+  }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def cut(tmp_path_factory):
+    """cut(d, kv_heads, group, m, width, block, causal, rows, max_q): the choice as a dict."""
+    at = tmp_path_factory.mktemp("cut")
+    src, exe = str(at / "cut.hip"), str(at / "cut")
+    with open(src, "w") as f:
+        f.write(PROBE)
+    subprocess.run([B.HIPCC, "--offload-host-only", "-std=c++17", "-O1", "-w", "-I", CSRC, "-I", INCLUDE, src, "-o", exe],
+                   check=True, capture_output=True)
+
+    def run(d, kv_heads, group, m, width, block=64, causal=True, rows=None, max_q=None):
+        sizes = (d, kv_heads, kv_heads * group, rows or sum(m), len(m), width, block, max_q or max(m), int(causal))
+        words = subprocess.run([exe], input=" ".join(map(str, sizes)), capture_output=True, text=True, check=True).stdout.split()
+        return dict(zip(words[::2], map(int, words[1::2])))
+
+    return run
+
+
+# d = 128 with tiles of 256 rows and requests of few rows in their grid: queries,
+# cached tokens, cached heads, heads to each, table's width, causal; tiles found
+# by number, the few rows' axis in parts, the tiles' axis in parts
+MIXED = [
+    ([700, 2, 700, 31], [4000, 3900, 2000, 4096], 2, 3, 64, False, True, True, True),
+    ([900, 5, 900], [2900, 2941, 901], 2, 3, 46, True, True, True, True),
+    ([600, 600, 3, 600], [2900, 600, 3001, 0], 2, 3, 52, True, False, True, True),
+    ([1000, 600, 3, 1000], [2000, 700, 1999, 1000], 30, 2, 32, True, True, False, False),
+    ([600, 3, 1, 600, 0, 600, 9, 600, 600, 600, 600, 600], [900, 1000, 1, 600] + [601, 1024, 77] + [620] * 5, 30, 2, 16, False,
+     False, False, False),
+]
+
+
+@pytest.mark.parametrize("case", range(len(MIXED)))
+def test_large_tiles_with_few_rows_beside_them_are_chosen(cut, case):
+    m, kv, kv_heads, group, width, causal, numbered, few_parts, many_parts = MIXED[case]
+    c = cut(128, kv_heads, group, m, width, causal=causal, rows=sum(m) + 1)
+    assert min(x * group for x in m if x) <= 32 and max(kv) <= 64 * width
+    assert c["tile_rows"] == 256 and (c["items"] > 0) == numbered
+    assert (c["few_chunks"] > 1) == few_parts and (c["many_chunks"] > 1) == many_parts
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", range(len(MIXED)))
+def test_large_tiles_with_few_rows_beside_them(case):
+    m, kv, kv_heads, group, width, causal = MIXED[case][:6]
+    pages = sum(-(-n // 64) for n in kv) + 1
+    pool = _filled(pages, kv_heads, 128, 64, case)
+    start = [0] + np.cumsum(m).tolist()
+    q = _bf16(start[-1] + 1, kv_heads * group, 128, seed=case + 3)
+    _check_attn(q, pool, _tables(kv, 64, pages, case, width=width), start, kv, 64, causal)

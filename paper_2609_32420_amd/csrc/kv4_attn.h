@@ -85,7 +85,7 @@ struct Cut {
   int span;   // rows of a request and cached head that parts are kept for; 0: parts are kept by query row
   __device__ bool has(const Span &s) const { return s.rows > over && s.rows <= upto; }
 };
-constexpr int kFindBatch = 1024;  // requests among which a tile is found by its number
+constexpr int kFindBatch = 1024;  // requests among which a tile is found by its number at a time
 // Workgroups of a cut.
 inline int64_t tile_groups(const Kv4Attn &a, const Cut &cut) {
   return (cut.items ? (int64_t)cut.items : (int64_t)cut.turns * a.batch) * a.c.heads * cut.chunks;

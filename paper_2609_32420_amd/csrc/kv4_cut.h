@@ -154,12 +154,13 @@ inline Cut many_cut(const Kv4Attn &a, double *whole_us) {
   // Ragged batches: the turns hold many tiles that there are not, each a workgroup
   // that starts to find nothing; the rows leave at most `most` (a part of a tile a
   // request, of those with more than `over` rows).  Finding a tile by its number
-  // takes a workgroup half a microsecond.  A prompt of 4096 beside 30 single tokens,
-  // 16 / 4 heads, 8000 cached: d = 64 117 -> 94 us, d = 128 (with the choices above)
-  // 424 -> 103.
+  // takes a workgroup half a microsecond for each 1024 requests before it.  A prompt
+  // of 4096 beside 30 single tokens, 16 / 4 heads, 8000 cached: d = 64 117 -> 94 us,
+  // d = 128 (with the choices above) 424 -> 103; one of 8192 beside 1024, 32 / 8
+  // heads, d = 64, a table for 16,384: 7461 -> 541.
   const int64_t rows = (int64_t)a.n_rows * a.group, some = rows / (cut.over + 1);
   const int64_t most = rows / cut.tile_rows + (some < a.batch ? some : a.batch);
-  if (a.batch > 1 && a.batch <= kFindBatch && 2 * (int64_t)cut.turns * a.batch > 3 * most) cut.items = (int)(most ? most : 1);
+  if (a.batch > 1 && 2 * (int64_t)cut.turns * a.batch > 3 * most) cut.items = (int)(most ? most : 1);
   return cut;
 }
 

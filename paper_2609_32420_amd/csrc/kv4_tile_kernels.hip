@@ -85,18 +85,19 @@ __device__ inline int wave_sum(int x) {
   return __builtin_amdgcn_readlane(x, 63);
 }
 
-// Turn and request of tile `item` in the order of the turns, where a request has
-// `late` empty ones before its tiles; request -1 behind the last tile.  A lane
-// holds the requests lane + 64 k, k < K.
+// Turn and request of tile `item` of the requests from base on (64 K of them) in the
+// order of the turns, where a request has `late` empty ones before its tiles;
+// request -1, and item counted down, where it lies behind their last.  A lane
+// holds the requests base + lane + 64 k, k < K.
 template <int ROWS, int K>
-__device__ inline int2 find_tile(const Kv4Attn &a, const Cut &cut, int item) {
+__device__ inline int2 find_tile(const Kv4Attn &a, const Cut &cut, int base, int &item) {
   const int lane = threadIdx.x & 63;
   int n[K], late[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     n[k] = late[k] = 0;
-    const int b = lane + 64 * k;
-    if (64 * k < a.batch && b < a.batch) {
+    const int b = base + lane + 64 * k;
+    if (base + 64 * k < a.batch && b < a.batch) {
       const Span sp = lane_span_of(a, b);
       if (cut.has(sp)) n[k] = (sp.rows + ROWS - 1) / ROWS;
       late[k] = late_of<ROWS>(a, cut, sp);
@@ -106,11 +107,15 @@ __device__ inline int2 find_tile(const Kv4Attn &a, const Cut &cut, int item) {
     int s = 0;
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (64 * k < a.batch) s += min(max(t - late[k], 0), n[k]);
+      if (base + 64 * k < a.batch) s += min(max(t - late[k], 0), n[k]);
     return wave_sum(s);
   };
   int t = 0, end = cut.turns, first = 0;
-  if (item >= before(end)) return make_int2(0, -1);
+  const int all = before(end);
+  if (item >= all) {
+    item -= all;
+    return make_int2(0, -1);
+  }
   while (end - t > 1) {  // before(t) <= item < before(end)
     const int mid = (t + end) >> 1, s = before(mid);
     if (s <= item) {
@@ -123,12 +128,12 @@ __device__ inline int2 find_tile(const Kv4Attn &a, const Cut &cut, int item) {
   int left = item - first, b = -1;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    if (64 * k >= a.batch) break;
+    if (base + 64 * k >= a.batch) break;
     const uint64_t in = __ballot(t >= late[k] && t - late[k] < n[k]);
     const int count = __builtin_popcountll(in);
     if (b < 0 && left < count) {
       const int rank = __builtin_amdgcn_mbcnt_hi((unsigned)(in >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in, 0));
-      b = 64 * k + __builtin_ctzll(__ballot((in >> lane & 1) && rank == left));
+      b = base + 64 * k + __builtin_ctzll(__ballot((in >> lane & 1) && rank == left));
     }
     left -= count;
   }
@@ -162,7 +167,14 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, int few_first, Cut cut, Parts p
   id /= a.c.heads;
   int b, chunk = id;
   if (cut.items) {
-    const int2 found = a.batch <= 64 ? find_tile<ROWS, 1>(a, cut, turn_of) : find_tile<ROWS, kFindBatch / 64>(a, cut, turn_of);
+    int2 found;
+    if (a.batch <= 64) {
+      found = find_tile<ROWS, 1>(a, cut, 0, turn_of);
+    } else {
+      found = find_tile<ROWS, kFindBatch / 64>(a, cut, 0, turn_of);
+      for (int base = kFindBatch; found.y < 0 && base < a.batch; base += kFindBatch)
+        found = find_tile<ROWS, kFindBatch / 64>(a, cut, base, turn_of);
+    }
     turn_of = found.x;
     b = found.y;
     if (b < 0) return;

@@ -83,3 +83,43 @@ def test_large_tiles_with_few_rows_beside_them(case):
     start = [0] + np.cumsum(m).tolist()
     q = _bf16(start[-1] + 1, kv_heads * group, 128, seed=case + 3)
     _check_attn(q, pool, _tables(kv, 64, pages, case, width=width), start, kv, 64, causal)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("batch", [900, 1024, 1025, 2048, 4096, 16384])
+def test_workgroups_of_a_ragged_batch_follow_its_tiles(cut, d, batch):
+    # a prompt of 8192 beside single tokens, 32 / 8 heads, a table for 16,384
+    m = [8192] + [1] * (batch - 1)
+    c = cut(d, 8, 4, m, 256)
+    # tiles of the rows that there are, a started one a request, the requests of few rows
+    assert c["groups"] <= 8 * c["many_chunks"] * (4 * sum(m) // c["tile_rows"] + batch) + max(8 * batch, 8192)
+    assert c["groups"] < 1 << 23
+
+
+def _many_requests(batch):
+    """Queries and cached tokens: the tiles lie in every 1024 requests, the longest prompt is the last."""
+    rng = np.random.default_rng(batch)
+    m = np.where(rng.random(batch) < 0.1, rng.integers(33, 180, batch), rng.integers(0, 3, batch))
+    m[-1] = 700
+    kv = np.where(rng.random(batch) < 0.2, 0, m + rng.integers(0, 60, batch))
+    kv[-1] = 900
+    return m.tolist(), kv.tolist()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("batch", [1100, 2048, 4100])
+def test_tiles_of_many_requests_are_found_by_number(cut, d, causal, batch):
+    m, kv = _many_requests(batch)
+    assert cut(d, 3, 1, m, max(-(-n // 64) for n in kv), causal=causal, rows=sum(m) + 1)["items"] > 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("batch,causal", [(1100, True), (1100, False), (2048, True), (4100, True)])
+def test_attention_of_many_requests(d, batch, causal):
+    m, kv = _many_requests(batch)
+    pages = sum(-(-n // 64) for n in kv)
+    pool = _filled(pages, 3, d, 64, 6)
+    start = [0] + np.cumsum(m).tolist()
+    _check_attn(_bf16(start[-1] + 1, 3, d, seed=d), pool, _tables(kv, 64, pages, 5), start, kv, 64, causal)

@@ -81,14 +81,14 @@ struct Cut {
   int tile_rows, tiles, chunk, chunks;
   int turns;  // of the kernel for many rows: a turn is a tile of every request
   int items;  // tiles of its grid, each found in the turns by its number; 0: the grid holds the turns
-  int columns;  // of requests of few rows: the grid holds parts 0 to columns - 1, a workgroup takes every columns-th
+  int columns;  // parts that the grid holds, and results of a row: a workgroup takes every columns-th of the chunks
   int span;   // rows of a request and cached head that parts are kept for; 0: parts are kept by query row
   __device__ bool has(const Span &s) const { return s.rows > over && s.rows <= upto; }
 };
 constexpr int kFindBatch = 1024;  // requests among which a tile is found by its number at a time
 // Workgroups of a cut.
 inline int64_t tile_groups(const Kv4Attn &a, const Cut &cut) {
-  return (cut.items ? (int64_t)cut.items : (int64_t)cut.turns * a.batch) * a.c.heads * cut.chunks;
+  return (cut.items ? (int64_t)cut.items : (int64_t)cut.turns * a.batch) * a.c.heads * cut.columns;
 }
 // Empty turns before a request's tiles: those of a request that ends `late` tiles'
 // tokens before the table does are that much later, so that a causal batch goes by
@@ -97,7 +97,7 @@ template <int ROWS>
 __device__ inline int late_of(const Kv4Attn &a, const Cut &cut, const Span &s) {
   return cut.turns > cut.tiles ? (int)((int64_t)((a.width << a.c.shift) - s.kv) * a.group / ROWS) : 0;
 }
-// Results of the parts: outputs [..][chunks][d] not yet divided, (reference,
+// Results of the parts: outputs [..][columns][d] not yet divided, (reference,
 // rounded sum, sum) beside them, by query row and head or, where that is less (a
 // padded batch, or one of few rows to a request), by request, cached head and row.
 struct Parts {
@@ -105,7 +105,7 @@ struct Parts {
   float4 *ml;
 };
 __device__ inline int64_t part_of(const Kv4Attn &a, const Cut &cut, const Span &s, int b, int h, int row, int i, int hd) {
-  return (cut.span ? ((int64_t)b * a.c.heads + h) * cut.span + row : (int64_t)(s.q0 + i) * a.heads + hd) * cut.chunks;
+  return (cut.span ? ((int64_t)b * a.c.heads + h) * cut.span + row : (int64_t)(s.q0 + i) * a.heads + hd) * cut.columns;
 }
 
 // The kernel for many rows (kv4_tile_kernels.hip), without the joining; its first or

@@ -8,7 +8,7 @@ namespace carnator {
 namespace {
 
 template <int D, int NT, bool SPLIT>
-__global__ void __launch_bounds__(64 * kWaves, NT == 1 ? 3 : 2)
+__global__ void __launch_bounds__(64 * kWaves, NT * D <= 128 ? 3 : 2)
 rows_kernel(Kv4Attn a, Cut cut, Parts parts) {
   extern __shared__ float lds_rows[];
   rows_body<D, NT, SPLIT, kWaves>(a, cut, parts, (int)blockIdx.x, lds_rows);
@@ -55,7 +55,7 @@ join_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut many, Parts many_parts, int
   const int row = i * a.group + hd % a.group;
   const int end = tile_end(a, sp, row - row % cut.tile_rows, cut.tile_rows);
   if (end <= cut.chunk) return;
-  const int n = (end + cut.chunk - 1) / cut.chunk;
+  const int n = min((end + cut.chunk - 1) / cut.chunk, cut.columns);
   const int64_t at = part_of(a, cut, sp, b, hd / a.group, row, i, hd);
   constexpr int EARLY = SHORT ? kShortJoin / kWaves : 1;
   float4 first = make_float4(-INFINITY, 0.f, 0.f, 0.f);
@@ -140,7 +140,7 @@ join_few_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut many, Parts many_parts,
   const int row = i * a.group + hd % a.group;
   const int end = tile_end(a, sp, row - row % cut.tile_rows, cut.tile_rows);
   if (end <= cut.chunk) return;
-  const int n = (end + cut.chunk - 1) / cut.chunk;
+  const int n = min((end + cut.chunk - 1) / cut.chunk, cut.columns);
   const int64_t at = part_of(a, cut, sp, b, hd / a.group, row, i, hd);
   float m = -INFINITY, l = 0.f, le = 0.f;
   f32x4 o = {};
@@ -202,13 +202,13 @@ hipError_t launch_join(const Kv4Attn &a, const Cut &few, const Parts &fp, const 
   const int64_t n = join.queries * a.heads;
   const int most = join.most;
   const bool d128 = a.c.d == 128;
-  const int parts = many.tiles > 0 && many.chunks > 1 ? many.chunks : few.chunks;
+  const int parts = many.tiles > 0 && many.columns > 1 ? many.columns : few.columns;
   if (parts <= 16 && n >= 2048) {
     const dim3 grid((unsigned)up(n, 1024 / a.c.d));
     if (d128) hipLaunchKernelGGL(join_few_kernel<128>, grid, dim3(256), 0, s, a, few, fp, many, mp, most);
     else hipLaunchKernelGGL(join_few_kernel<64>, grid, dim3(256), 0, s, a, few, fp, many, mp, most);
   } else {
-    const bool is_short = (many.tiles > 0 && many.chunks > few.chunks ? many.chunks : few.chunks) <= kShortJoin;
+    const bool is_short = (many.tiles > 0 && many.columns > few.columns ? many.columns : few.columns) <= kShortJoin;
     const auto f = d128 ? (is_short ? &join_kernel<128, true> : &join_kernel<128, false>)
                         : (is_short ? &join_kernel<64, true> : &join_kernel<64, false>);
     hipLaunchKernelGGL(f, dim3((unsigned)n), dim3(64 * kWaves), 0, s, a, few, fp, many, mp, most);

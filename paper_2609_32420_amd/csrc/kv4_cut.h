@@ -55,8 +55,12 @@ inline void set_span(const Kv4Attn &a, Cut &cut, int64_t rows) {
 // 4000 cached 113 -> 103 us.
 // A table may be far wider than what is cached: of more than 8192 workgroups, some
 // thousand of which start to find nothing in a microsecond, the grid holds the
-// first parts, and a workgroup goes on to later ones.  48 requests of 1000 tokens,
-// 32 / 8 heads, d = 128, a table for 131,072: 43.6 us without, 18.6 so.
+// first parts, and a workgroup goes on to later ones with its running sums, so that
+// results number the workgroups; past 4096 requests and heads the axis is whole.
+// 48 requests of 1000 tokens, 32 / 8 heads, d = 128, a table for 131,072: 43.6 us
+// without, 18.6 so.  With a result for every part instead, 200 requests of 600
+// tokens take 39.7 us (now 34.0) and 291 MB of scratch (17), 600 of up to 8000
+// under a tight table 354 (296) and 61 MB (none).
 inline Cut few_cut(const Kv4Attn &a, double many_us) {
   const int64_t rows = most_rows(a) < few_rows(a) ? most_rows(a) : few_rows(a);
   const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
@@ -67,9 +71,10 @@ inline Cut few_cut(const Kv4Attn &a, double many_us) {
   if (reach <= 512 || (reach <= 1024 && base > 64) ||
       (reach <= 8192 && 2 * 0.7 / 128 * (double)reach <= many_us))
     return cut;
+  const int64_t columns = kFewGroups / base;
+  if (columns < 2) return cut;
   const int64_t chunk = up(up(reach * base, 640), 128) * 128;
   set_chunk(cut, reach, chunk > 1536 ? 1536 : chunk);
-  const int64_t columns = kFewGroups / base > 1 ? kFewGroups / base : 1;
   cut.columns = (int)(cut.chunks < columns ? cut.chunks : columns);
   return cut;
 }
@@ -108,7 +113,7 @@ constexpr double kTokenUs[3][3] = {{0.0146, 0.019, 0.0286}, {0.020, 0.027, 0.027
 inline Cut many_cut(const Kv4Attn &a, double *whole_us) {
   *whole_us = 0;
   const int64_t reach = (int64_t)a.width << a.c.shift;
-  Cut cut{few_rows(a), 0x7FFFFFFF, 128, 0, (int)reach, 1, 0, 0, 0, 0};
+  Cut cut{few_rows(a), 0x7FFFFFFF, 128, 0, (int)reach, 1, 0, 0, 1, 0};
   if (most_rows(a) <= few_rows(a)) return cut;
   set_span(a, cut, most_rows(a));
   if (a.batch == 1) cut.over = 0;  // a single request is left to this kernel however few rows it has
@@ -143,7 +148,7 @@ inline Cut many_cut(const Kv4Attn &a, double *whole_us) {
         cut.tile_rows = rows;
         cut.tiles = (int)tiles;
         cut.chunk = (int)chunk;
-        cut.chunks = (int)up(reach, chunk);
+        cut.chunks = cut.columns = (int)up(reach, chunk);
       }
     }
   }
@@ -175,11 +180,11 @@ inline Cuts cuts(const Kv4Attn &a) {
 
 // Scratch of a cut: the parts' outputs, then their references and sums.
 inline size_t part_count(const Kv4Attn &a, const Cut &cut) {
-  return (cut.span ? (size_t)cut.span * a.batch * a.c.heads : (size_t)a.n_rows * a.heads) * cut.chunks;
+  return (cut.span ? (size_t)cut.span * a.batch * a.c.heads : (size_t)a.n_rows * a.heads) * cut.columns;
 }
 inline size_t outputs_bytes(const Kv4Attn &a, const Cut &cut) { return align_up(part_count(a, cut) * a.c.d * 4); }
 inline size_t parts_bytes(const Kv4Attn &a, const Cut &cut) {
-  if (cut.chunks == 1 || cut.tiles == 0) return 0;
+  if (cut.columns == 1 || cut.tiles == 0) return 0;
   return outputs_bytes(a, cut) + align_up(part_count(a, cut) * 16);
 }
 // Queries that a second kernel looks at, and of them `most` to a request (0: by row).

@@ -41,23 +41,21 @@ struct Raw {
   uint2 vs[D / 64];  // the octet's scales
 };
 
-// Part `chunk` (0 unless SPLIT) of request b, cached head h.
+// Request b, cached head h; SPLIT: of its key axis the parts column, column +
+// cut.columns, .. in turn, under one running maximum and sum.
 template <int D, int NT, bool SPLIT, int WAVES>
 __device__ __attribute__((always_inline)) inline void rows_part(const Kv4Attn &a, const Cut &cut, const Parts &parts,
-                                                                const Span &sp, int b, int h, int chunk, float *lds_o) {
+                                                                const Span &sp, int b, int h, int column, float *lds_o) {
   constexpr int TQ = D / 32;        // products of a key tile
   constexpr int CPL = D / 4;        // channels of a lane
   constexpr int NV = D / 64;        // 64-channel parts of V
   // lds_o: [WAVES / 2][NT * NV * 16][64] outputs, then [WAVES / 2][NT][3][64] references and sums
-  int tid = threadIdx.x;
-  if constexpr (SPLIT) asm volatile("" : "+v"(tid));  // what follows from it is not kept over rows_body's loop
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, j = lane >> 4;
   constexpr int row0 = 0;
   const int end = tile_end(a, sp, row0, 16 * NT);  // tokens that a row of the tile sees
-  const int k_first = SPLIT ? chunk * cut.chunk : 0;
   const bool whole = !SPLIT || end <= cut.chunk;  // nothing to join
-  const int k_end = SPLIT ? min(end, k_first + cut.chunk) : end;
+  int part = SPLIT ? column * cut.chunk : 0, part_end = SPLIT ? min(end, part + cut.chunk) : end;
   const int seen_by_all = sp.limit(a, row0 / a.group);
 
   // ---- Q: query column r of each 16, channels CPL j + 8 t .. + 8
@@ -96,7 +94,7 @@ __device__ __attribute__((always_inline)) inline void rows_part(const Kv4Attn &a
   const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
 
   // ---- the wave's steps: pages come from the table 64 entries at a time
-  int entry0 = k_first >> a.c.shift;  // of lane 0
+  int entry0 = part >> a.c.shift;  // of lane 0
   int entry = -1;
   auto look = [&]() {
     entry = -1;
@@ -104,9 +102,17 @@ __device__ __attribute__((always_inline)) inline void rows_part(const Kv4Attn &a
   };
   look();
   int page = -1;
-  // the first of the wave's steps from k0 on that has a page
+  // the first of the wave's steps from k0 on that has a page; end and beyond: none
   auto next = [&](int k0) {
-    for (; k0 < k_end; k0 += WAVES * kStep) {
+    for (; k0 < end; k0 += WAVES * kStep) {
+      if constexpr (SPLIT) {
+        while (k0 >= part_end) {  // on to the workgroup's next part
+          part = (int)min((unsigned)part + (unsigned)(cut.columns * cut.chunk), (unsigned)end);
+          if (part == end) return end;
+          part_end = min(end, part + cut.chunk);
+          k0 = part + wave * kStep;
+        }
+      }
       int at = (k0 >> a.c.shift) - entry0;
       if (at >= 64) {
         entry0 += at;
@@ -267,19 +273,19 @@ __device__ __attribute__((always_inline)) inline void rows_part(const Kv4Attn &a
   // the loads of a step are under way during the one before
   Raw<D> even, odd;
   const int stride = WAVES * kStep;
-  int k0 = next(k_first + wave * kStep);
-  if (k0 < k_end) {
+  int k0 = next(part + wave * kStep);
+  if (k0 < end) {
     load(even, k0);
     int k1 = next(k0 + stride);
-    while (k1 < k_end) {
+    while (k1 < end) {
       load(odd, k1);
       step(even, k0);
       k0 = next(k1 + stride);
-      if (k0 < k_end) load(even, k0);
+      if (k0 < end) load(even, k0);
       step(odd, k1);
       k1 = next(k0 + stride);
     }
-    if (k0 < k_end) step(even, k0);
+    if (k0 < end) step(even, k0);
   }
   // ---- sums over the lanes of a query, then the waves' parts in a fixed order
 #pragma unroll
@@ -343,7 +349,7 @@ __device__ __attribute__((always_inline)) inline void rows_part(const Kv4Attn &a
     if (row >= sp.rows) continue;
     const int i = row / a.group, hd = h * a.group + row - i * a.group;
     if (SPLIT && !whole) {
-      const int64_t at = part_of(a, cut, sp, b, h, row, i, hd) + chunk;
+      const int64_t at = part_of(a, cut, sp, b, h, row, i, hd) + column;
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -380,15 +386,9 @@ __device__ __attribute__((always_inline)) inline void rows_body(const Kv4Attn &a
   if constexpr (!SPLIT) {
     rows_part<D, NT, false, WAVES>(a, cut, parts, sp, b, h, 0, lds_o);
   } else {
-    const int end = tile_end(a, sp, 0, 16 * NT);
-    int chunk = id / a.batch;
-    if (chunk > 0 && chunk * cut.chunk >= end) return;
-    for (;;) {
-      rows_part<D, NT, true, WAVES>(a, cut, parts, sp, b, h, chunk, lds_o);
-      chunk += cut.columns;
-      if (chunk >= cut.chunks || chunk * cut.chunk >= end) return;
-      __syncthreads();  // LDS is free again
-    }
+    const int column = id / a.batch;
+    if (column > 0 && column * cut.chunk >= tile_end(a, sp, 0, 16 * NT)) return;
+    rows_part<D, NT, true, WAVES>(a, cut, parts, sp, b, h, column, lds_o);
   }
 }
 

@@ -5,10 +5,11 @@ import subprocess
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2609_32420_amd as P
 from paper_2609_32420_amd import build as B
-from test_gpu_kv4 import _bf16, _check_attn, _filled, _tables
+from test_gpu_kv4 import DEV, _bf16, _check_attn, _filled, _tables
 
 CSRC = os.path.join(os.path.dirname(P.__file__), "csrc")
 INCLUDE = os.path.join(B.ROOT, "include")
@@ -26,9 +27,9 @@ int main() {
     a.heads = (int)heads, a.group = (int)(heads / kv_heads), a.n_rows = (int)rows, a.batch = (int)batch;
     a.width = (int)width, a.max_q = (int)(max_q < rows ? max_q : rows), a.causal = (int)causal;
     const auto [few, many] = cuts(a);
-    printf("tile_rows %d few_chunks %d many_tiles %d many_chunks %d turns %d items %d bytes %zu groups %lld\n",
-           many.tile_rows, few.chunks, many.tiles, many.chunks, many.turns, many.items,
-           parts_bytes(a, few) + parts_bytes(a, many), (long long)(few_groups(a, few) + tile_groups(a, many)));
+    printf("tile_rows %d few_chunks %d few_columns %d many_tiles %d many_chunks %d turns %d items %d few_bytes %zu many_bytes %zu "
+           "groups %lld\n", many.tile_rows, few.chunks, few.columns, many.tiles, many.chunks, many.turns, many.items,
+           parts_bytes(a, few), parts_bytes(a, many), (long long)(few_groups(a, few) + tile_groups(a, many)));
   }
 }
 """
@@ -123,3 +124,58 @@ def test_attention_of_many_requests(d, batch, causal):
     pool = _filled(pages, 3, d, 64, 6)
     start = [0] + np.cumsum(m).tolist()
     _check_attn(_bf16(start[-1] + 1, 3, d, seed=d), pool, _tables(kv, 64, pages, 5), start, kv, 64, causal)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_parts_of_few_rows_follow_their_workgroups(cut, d):
+    # at most 8192 workgroups write parts, each of 64 (d = 64) or 32 rows of d outputs
+    # and 16 bytes beside them, whatever the table's width; one alone writes none
+    most = 8192 * (64 * (64 * 4 + 16) if d == 64 else 32 * (128 * 4 + 16)) + 512
+    for m, kv_heads, group, width in [
+            ([1] * 1024, 8, 4, 2048), ([4] * 256, 8, 8, 2048), ([8192] + [1] * 1023, 8, 4, 256), ([8000] + [1] * 1499, 8, 4, 512),
+            ([100000] + [1] * 60, 8, 4, 2048), ([100000] + [1] * 1023, 8, 4, 2048), ([1], 8, 4, 1 << 20), ([8] * 900, 1, 8, 1 << 20),
+            ([32] * 100, 12, 1, 4096), ([64, 63] * 32, 8, 1, 4096), ([1] * 16384, 12, 2, 2048), ([1, 2, 1] * 341, 4, 8, 300)]:
+        c = cut(d, kv_heads, group, m, width)
+        assert c["few_bytes"] <= most, (m[:3], c)
+        if len(m) * kv_heads > 4096:
+            assert c["few_chunks"] == 1 and c["few_bytes"] == 0
+
+
+IN_TURN = [(1, 1), (3, 1), (20, 1), (1, 9), (3, 9), (1, 30), (2, 7), (40, 1)]  # queries at most, heads to a cached one
+
+
+def _in_turn(most):
+    """Queries of 40 requests (four have any) and their cached tokens."""
+    m, kv = [0] * 40, [1 + 3 * b for b in range(40)]
+    m[0], m[3], m[20], m[33] = 1, most, min(most, 2), 1
+    kv[0], kv[3], kv[9], kv[20] = 9000, 8100, 8192, 4700
+    return m, kv
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("most,group", IN_TURN)
+def test_workgroups_take_parts_in_turn(cut, d, most, group):
+    m, kv = _in_turn(most)
+    c = cut(d, 60, group, m, 1024)
+    assert 1 < c["few_columns"] < -(-max(kv) // 1536) and c["few_chunks"] == -(-65536 // 1536)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("most,group", IN_TURN)
+def test_parts_that_a_workgroup_takes_in_turn(d, most, group):
+    # tables far wider than the cache, so that a workgroup takes parts far apart under
+    # one running sum; pages left out, also at a part's begin; scores that climb and fall
+    # from part to part
+    kv_heads = 60
+    m, kv = _in_turn(most)
+    pages = sum(-(-n // 64) for n in kv)
+    pool = P.kv4_pool(pages, kv_heads, d, 64)
+    n = pages * 64
+    k = _bf16(n, kv_heads, d, seed=group).float() + 3 * torch.sin(torch.arange(n, device=DEV) / 700)[:, None, None]
+    P.kv4_store(pool, k.to(torch.bfloat16), _bf16(n, kv_heads, d, seed=2), torch.arange(n, dtype=torch.int32, device=DEV), 64)
+    table = _tables(kv, 64, pages, 5, width=1024)
+    table[3, 0:3] = table[0, 24] = table[0, 90:] = -1
+    start = [0] + np.cumsum(m).tolist()
+    q = (_bf16(start[-1], kv_heads * group, d, seed=d).float() + 1).to(torch.bfloat16)
+    _check_attn(q, pool, table, start, kv, 64, most == 3)

@@ -352,7 +352,8 @@ int carnator_select_block_mask(const double *mass, const carnator_shape *shape,
  *               q_start[0] and behind q_start[batch] are left untouched; may
  *               not alias q or the pages
  *   lse         fp32 [n_rows, heads] contiguous, or NULL
- *   workspace   carnator_kv4_attn_workspace_size bytes, 256-byte aligned
+ *   workspace   carnator_kv4_attn_workspace_size bytes (below 2^30, whatever
+ *               the sizes), 256-byte aligned
  * heads a multiple of kv_heads; n_rows may be 0.
  * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED, E_ALIGN, E_WORKSPACE, E_HIP.
  */

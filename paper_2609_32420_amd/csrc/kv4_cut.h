@@ -8,6 +8,12 @@ namespace carnator {
 
 constexpr int kMaxParts = 64;     // parts of the requests of many rows
 constexpr int kFewGroups = 8192;  // workgroups for the requests of few rows
+// Bytes for the parts of the requests of many rows: 1.5 million rows' at d = 128 (23
+// rounds of workgroups), of whose parts the best number gains little.  us with any
+// number / so / with a third of it: 24 heads, 12,270 queries, 100,000 tokens 14,400 /
+// 14,400 / 15,450; 12 heads, 2 requests of 3615, 107,000 tokens 4970 / 4970 / 5380;
+// 32 / 8 heads, 8 of 4096 over 5000 tokens, a table for 131,072, 1820 / 1670 / 1670.
+constexpr int64_t kPartsBytes = (int64_t)3 << 28;
 
 // Workgroups for the requests of few rows.
 inline int64_t few_groups(const Kv4Attn &a, const Cut &cut) { return (int64_t)a.batch * a.c.heads * cut.columns; }
@@ -121,6 +127,8 @@ inline Cut many_cut(const Kv4Attn &a, double *whole_us) {
   const bool ragged = (int64_t)a.max_q * a.batch > a.n_rows;
   const int64_t long_ones = a.n_rows / a.max_q;
   const bool large = d128 && (!ragged || a.batch <= 4 * long_ones);
+  const int64_t part_bytes = (cut.span ? (int64_t)cut.span * a.batch * a.c.heads : (int64_t)a.n_rows * a.heads) *
+                             (4 * a.c.d + 16);
   double best = 1e300;
   for (int rows = 128; rows <= (large ? 256 : 128); rows *= 2) {
     const int64_t tiles = up(most_rows(a), rows);
@@ -133,7 +141,7 @@ inline Cut many_cut(const Kv4Attn &a, double *whole_us) {
     const int fit = rows == 256 ? 1 : d128 ? 2 : 3;  // workgroups on a CU
     const double *token = kTokenUs[rows == 256 ? 2 : d128];
     const double start = rows != 256 ? 0 : ragged ? 8 : 4, part = (d128 ? 0.03 : 0.015) * (ragged ? 1.3 : 1);
-    for (int64_t n = 1; n <= kMaxParts && (n == 1 || reach >= n * 128); ++n) {
+    for (int64_t n = 1; n <= kMaxParts && (n == 1 || (reach >= n * 128 && n * part_bytes <= kPartsBytes)); ++n) {
       const int64_t chunk = n == 1 ? reach : up(up(reach, n), 128) * 128;
       const int64_t groups = base * n, round = 256 * fit;
       const int64_t on_cu = up(groups, 256) < fit ? up(groups, 256) : fit;

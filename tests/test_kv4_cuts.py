@@ -1,5 +1,6 @@
 """How attention over 4-bit cached keys and values is cut into workgroups: the
 host's choice (no GPU) for the sizes that the GPU tests below run."""
+import ctypes
 import os
 import subprocess
 
@@ -179,3 +180,27 @@ def test_parts_that_a_workgroup_takes_in_turn(d, most, group):
     start = [0] + np.cumsum(m).tolist()
     q = (_bf16(start[-1], kv_heads * group, d, seed=d).float() + 1).to(torch.bfloat16)
     _check_attn(q, pool, table, start, kv, 64, most == 3)
+
+
+def _workspace(d, kv_heads, group, m, width, block=64):
+    c = P.Kv4(0x100000, 1 << 20, kv_heads, d, block)
+    return P.lib().carnator_kv4_attn_workspace_size(ctypes.byref(c), kv_heads * group, sum(m), len(m), width, max(m))
+
+
+def test_workspaces_are_bounded():
+    # 3 * 2^28 bytes for the parts of many rows, 143 MB for those of few: below 2^30 together
+    for d in (64, 128):
+        for m, kv_heads, group, width in [
+                ([4096] * 8, 8, 4, 2048), ([8192] + [1] * 1023, 8, 4, 256), ([100000] + [1] * 60, 8, 4, 2048),
+                ([8000] + [1] * 1499, 8, 4, 512), ([32760], 12, 1, 512), ([119056], 24, 1, 1 << 20), ([500] * 1000, 8, 8, 1 << 14)]:
+            assert _workspace(d, kv_heads, group, m, width) < 1 << 30
+    rng = np.random.default_rng(1)
+    for _ in range(1000):
+        batch = int(2 ** rng.uniform(0, 14))
+        most = int(2 ** rng.uniform(0, 17))
+        m = [most] + rng.integers(0, max(1, int(most * rng.random()) ** int(rng.integers(0, 2))) + 1, batch - 1).tolist()
+        kv_heads, group = int(2 ** rng.uniform(0, 6)), int(2 ** rng.uniform(0, 5))
+        if sum(m) * kv_heads * group >= 1 << 31:
+            continue
+        width = int(2 ** rng.uniform(0, 23))
+        assert _workspace(64 << int(rng.integers(0, 2)), kv_heads, group, m, width, 64 << int(rng.integers(0, 2))) < 1 << 30

@@ -237,7 +237,7 @@ hipError_t launch_kv4_attn(const Kv4Attn &a, void *scratch, hipStream_t s) {
   hipError_t e;
   const bool d128 = a.c.d == 128;
   if (many.tiles > 0)
-    e = launch_kv4_tiles(a, few, fp, many.over == 0 ? 0 : (int)few_groups(a, few), many, mp, s);
+    e = launch_kv4_tiles(a, few, fp, (int)few_groups(a, few), many, mp, s);
   else if (few.tile_rows == 16)
     e = d128 ? launch_rows<128, 1>(a, few, fp, s) : launch_rows<64, 1>(a, few, fp, s);
   else if (few.tile_rows == 32)

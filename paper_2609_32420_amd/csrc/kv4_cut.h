@@ -183,7 +183,8 @@ struct Cuts {
 inline Cuts cuts(const Kv4Attn &a) {
   double whole_us;
   const Cut many = many_cut(a, &whole_us);
-  return Cuts{few_cut(a, whole_us), many};
+  // with no request left to it, the cut of few rows has neither workgroups nor parts
+  return Cuts{many.over == 0 ? Cut{0, 0, 16, 0, many.chunk, 1, 0, 0, 0, 0} : few_cut(a, whole_us), many};
 }
 
 // Scratch of a cut: the parts' outputs, then their references and sums.
@@ -192,7 +193,7 @@ inline size_t part_count(const Kv4Attn &a, const Cut &cut) {
 }
 inline size_t outputs_bytes(const Kv4Attn &a, const Cut &cut) { return align_up(part_count(a, cut) * a.c.d * 4); }
 inline size_t parts_bytes(const Kv4Attn &a, const Cut &cut) {
-  if (cut.columns == 1 || cut.tiles == 0) return 0;
+  if (cut.columns <= 1 || cut.tiles == 0) return 0;
   return outputs_bytes(a, cut) + align_up(part_count(a, cut) * 16);
 }
 // Queries that a second kernel looks at, and of them `most` to a request (0: by row).

@@ -204,3 +204,13 @@ def test_workspaces_are_bounded():
             continue
         width = int(2 ** rng.uniform(0, 23))
         assert _workspace(64 << int(rng.integers(0, 2)), kv_heads, group, m, width, 64 << int(rng.integers(0, 2))) < 1 << 30
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_single_request_of_many_rows_pays_for_no_few(cut, d):
+    # 21 frames: the axis whole, no workspace; 256 queries: what the tiles' parts take
+    c = cut(d, 12, 1, [4680], 512, causal=False)
+    assert c["few_bytes"] == 0 and c["groups"] == 12 * c["many_tiles"] * c["many_chunks"]
+    c = cut(d, 12, 1, [256], 32)
+    assert c["many_chunks"] > 1 and c["few_bytes"] == 0 and c["groups"] == 12 * c["many_tiles"] * c["many_chunks"]
+    assert _workspace(d, 12, 1, [256], 32) == c["many_bytes"] == 256 * 12 * c["many_chunks"] * (4 * d + 16)

@@ -354,7 +354,8 @@ int carnator_select_block_mask(const double *mass, const carnator_shape *shape,
  *   lse         fp32 [n_rows, heads] contiguous, or NULL
  *   workspace   carnator_kv4_attn_workspace_size bytes (below 2^30, whatever
  *               the sizes), 256-byte aligned
- * heads a multiple of kv_heads; n_rows may be 0.
+ * heads a multiple of kv_heads; n_rows may be 0.  A launch of 2^32 threads is
+ * E_UNSUPPORTED: about 2^24 requests times cached heads, or 2^31 rows times heads.
  * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED, E_ALIGN, E_WORKSPACE, E_HIP.
  */
 typedef struct {

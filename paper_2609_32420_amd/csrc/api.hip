@@ -530,9 +530,9 @@ int carnator_block_sparse_attn_rows(const carnator_view *q, const carnator_view 
 
 namespace {
 
-// Tokens of a table's width, and threads of a launch (a HIP grid holds 2^32).
+// Tokens of a table's width, and threads of a launch (a HIP grid holds fewer than 2^32).
 constexpr int64_t kMaxReach = (int64_t)1 << 30;
-constexpr int64_t kMaxWorkgroups = ((int64_t)1 << 24) - 1;
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
 
 int check_block(int32_t block) {
   if (block != 64 && block != 128)
@@ -713,9 +713,10 @@ int carnator_kv4_attn(const carnator_rows *q, int32_t n_rows, int32_t heads, con
     return fail(CARNATOR_E_ALIGN, "table, q_start, kv_len and lse must be 4-byte aligned");
   Kv4Attn a = attn_of(cache, heads, n_rows, batch, width, max_q);
   a.causal = causal != 0;
-  if (kv4_attn_workgroups(a) > kMaxWorkgroups)
-    return fail(CARNATOR_E_UNSUPPORTED, "batch * kv_heads * max_q needs %lld workgroups; at most %lld",
-                (long long)kv4_attn_workgroups(a), (long long)kMaxWorkgroups);
+  const int64_t threads = kv4_attn_threads(a);
+  if (threads > kMaxThreads)
+    return fail(CARNATOR_E_UNSUPPORTED, "batch, kv_heads and n_rows need a launch of %lld threads; at most %lld",
+                (long long)threads, (long long)kMaxThreads);
   if ((rc = check_ws(workspace, ws_bytes, kv4_attn_scratch_bytes(a)))) return rc;
   a.q = to_rows(q);
   a.table = table;

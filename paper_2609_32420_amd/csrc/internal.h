@@ -235,8 +235,8 @@ struct Kv4Attn {
   int64_t ost, osh;
   float *lse;
 };
-// Largest launch of a call, and its scratch.
-int64_t kv4_attn_workgroups(const Kv4Attn &a);
+// Threads of a call's largest launch, and its scratch.
+int64_t kv4_attn_threads(const Kv4Attn &a);
 size_t kv4_attn_scratch_bytes(const Kv4Attn &a);
 hipError_t launch_kv4_attn(const Kv4Attn &a, void *scratch, hipStream_t s);
 

@@ -183,6 +183,7 @@ join_few_kernel(Kv4Attn a, Cut few, Parts few_parts, Cut many, Parts many_parts,
 
 template <int D, int NT>
 hipError_t launch_rows(const Kv4Attn &a, const Cut &cut, const Parts &parts, hipStream_t s) {
+  static_assert(kWaves == 4, "256 threads, as most_threads has them");
   const size_t lds = rows_lds(D, NT, kWaves);
   const int64_t grid = few_groups(a, cut);
   const auto f = cut.chunks > 1 ? &rows_kernel<D, NT, true> : &rows_kernel<D, NT, false>;
@@ -202,8 +203,7 @@ hipError_t launch_join(const Kv4Attn &a, const Cut &few, const Parts &fp, const 
   const int64_t n = join.queries * a.heads;
   const int most = join.most;
   const bool d128 = a.c.d == 128;
-  const int parts = many.tiles > 0 && many.columns > 1 ? many.columns : few.columns;
-  if (parts <= 16 && n >= 2048) {
+  if (joins_few(few, many, n)) {
     const dim3 grid((unsigned)up(n, 1024 / a.c.d));
     if (d128) hipLaunchKernelGGL(join_few_kernel<128>, grid, dim3(256), 0, s, a, few, fp, many, mp, most);
     else hipLaunchKernelGGL(join_few_kernel<64>, grid, dim3(256), 0, s, a, few, fp, many, mp, most);
@@ -218,12 +218,7 @@ hipError_t launch_join(const Kv4Attn &a, const Cut &few, const Parts &fp, const 
 
 }  // namespace
 
-int64_t kv4_attn_workgroups(const Kv4Attn &a) {
-  const auto [few, many] = cuts(a);
-  const int64_t main = few_groups(a, few) + tile_groups(a, many);
-  const int64_t join = joined(a, few, many).queries * a.heads;
-  return main > join ? main : join;
-}
+int64_t kv4_attn_threads(const Kv4Attn &a) { return most_threads(a, cuts(a)); }
 
 size_t kv4_attn_scratch_bytes(const Kv4Attn &a) {
   const auto [few, many] = cuts(a);

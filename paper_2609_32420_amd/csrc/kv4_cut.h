@@ -210,5 +210,17 @@ inline Joined joined(const Kv4Attn &a, const Cut &few, const Cut &many) {
   const int64_t all = (int64_t)most * a.batch;
   return 2 * all > 3 * (int64_t)a.n_rows ? Joined{a.n_rows, 0} : Joined{all, most};
 }
+// Whether n rows and heads are joined by the kernel for few parts of many.
+inline bool joins_few(const Cut &few, const Cut &many, int64_t n) {
+  return (many.tiles > 0 && many.columns > 1 ? many.columns : few.columns) <= 16 && n >= 2048;
+}
+
+// Threads of a call's largest launch.
+inline int64_t most_threads(const Kv4Attn &a, const Cuts &c) {
+  const int64_t main = (few_groups(a, c.few) + tile_groups(a, c.many)) * (c.many.tile_rows == 256 ? 512 : 256);
+  const int64_t n = joined(a, c.few, c.many).queries * a.heads;
+  const int64_t join = (joins_few(c.few, c.many, n) ? up(n, 1024 / a.c.d) : n) * 256;
+  return main > join ? main : join;
+}
 
 }  // namespace carnator

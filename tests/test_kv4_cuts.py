@@ -29,8 +29,9 @@ int main() {
     a.width = (int)width, a.max_q = (int)(max_q < rows ? max_q : rows), a.causal = (int)causal;
     const auto [few, many] = cuts(a);
     printf("tile_rows %d few_chunks %d few_columns %d many_tiles %d many_chunks %d turns %d items %d few_bytes %zu many_bytes %zu "
-           "groups %lld\n", many.tile_rows, few.chunks, few.columns, many.tiles, many.chunks, many.turns, many.items,
-           parts_bytes(a, few), parts_bytes(a, many), (long long)(few_groups(a, few) + tile_groups(a, many)));
+           "groups %lld threads %lld\n", many.tile_rows, few.chunks, few.columns, many.tiles, many.chunks, many.turns, many.items,
+           parts_bytes(a, few), parts_bytes(a, many), (long long)(few_groups(a, few) + tile_groups(a, many)),
+           (long long)most_threads(a, cuts(a)));
   }
 }
 """
@@ -214,3 +215,17 @@ def test_a_single_request_of_many_rows_pays_for_no_few(cut, d):
     c = cut(d, 12, 1, [256], 32)
     assert c["many_chunks"] > 1 and c["few_bytes"] == 0 and c["groups"] == 12 * c["many_tiles"] * c["many_chunks"]
     assert _workspace(d, 12, 1, [256], 32) == c["many_bytes"] == 256 * 12 * c["many_chunks"] * (4 * d + 16)
+
+
+def test_a_launch_of_2_32_threads_is_refused(cut):
+    # tiles of 256 rows have 512 threads
+    def call(rows, batch, most):
+        c, q = P.Kv4(0x100000, 4, 1, 128, 64), P.Rows(0x200000, 128, 128)
+        return P.lib().carnator_kv4_attn(ctypes.byref(q), rows, 1, ctypes.byref(c), 0x10000, batch, 512, 0x10000, 0x10000,
+                                         most, 0, 0.0, 0x60000, 128, 128, None, None, 0, None)
+
+    rows = (1 << 31) - 1
+    c = cut(128, 1, 1, [rows], 512)
+    assert c["tile_rows"] == 256 and c["groups"] < 1 << 24 and c["threads"] >= 1 << 32
+    assert call(rows, 1, rows) == -3 and b"threads" in P.lib().carnator_last_error()
+    assert call(1, 1 << 24, 1) == -3

@@ -862,13 +862,13 @@ class Kv4Cache:
         kv4_store do not).  Returns (q_start, positions, lacking): the rows'
         starts and positions, and the number of tokens without a page or an
         entry in the table, which are not held."""
+        before = self.table.clone()
         q_start, kv_len, slots, positions, counts = page_plan(self.kv_len, new_len, self.table, self.free, self.block,
                                                               k.shape[0])
         try:
             kv4_store(self.pool, k, v, slots, self.block)
         except Exception:  # refused: the pages entered in the table are still free
-            held = (self.kv_len + (self.block - 1)) // self.block
-            self.table[torch.arange(self.table.shape[1], device=self.table.device) >= held[:, None]] = -1
+            self.table.copy_(before)
             raise
         self.kv_len.copy_(kv_len)  # in place, as the table: a captured attention goes on reading it
         _, taken, lacking = counts.tolist()

@@ -1,0 +1,27 @@
+"""What a cache of keys and values in 4 bits does with the calls that its
+documentation allows and refuses (see test_gpu_kv4.py for its results)."""
+import pytest
+import torch
+
+import paper_2609_32420_amd as P
+from test_gpu_kv4 import _bf16, _i32
+
+
+@pytest.mark.gpu
+def test_a_refused_append_leaves_entries_made_ahead():
+    # pages of a history entered behind the lengths, in a request that gets tokens and in one that does not
+    heads, d = 1, 64
+    cache = P.Kv4Cache(9, 3, 5, heads, d, 64)
+    k = _bf16(140, heads, d, seed=1)
+    assert cache.append(k, k, _i32([70, 5, 65]))[2] == 0
+    cache.table[0, 3] = cache.table[2, 0]
+    cache.table[1, 1:4] = cache.table[0, :3]
+    before = cache.table.clone(), cache.kv_len.clone(), cache.free.clone()
+    odd = _bf16(91 * d + 4)[4:].view(91, heads, d)  # 8 bytes off
+    for v, error in ((k[:90].float(), ValueError), (k[:60], ValueError), (odd[:90], P.CarnatorError)):
+        with pytest.raises(error):
+            cache.append(k[:90], v, _i32([90, 0, 0]))
+        for got, want in zip((cache.table, cache.kv_len, cache.free), before):
+            assert torch.equal(got, want)
+    assert cache.append(k[:90], k[:90], _i32([90, 0, 0]))[2] == 0
+    assert torch.equal(cache.table[1:], before[0][1:]) and int(cache.kv_len[0]) == 160

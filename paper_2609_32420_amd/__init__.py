@@ -876,9 +876,10 @@ class Kv4Cache:
         return q_start, positions, lacking
 
     def release(self, requests) -> None:
-        """Empties the requests (indices); their pages that no other table row
-        names are free again."""
-        pages = self.table[requests].flatten()
+        """Empties the requests (an index, a slice, or a list or tensor of
+        indices or truth values); their pages that no other table row names
+        are free again."""
+        pages = self.table[requests].flatten().clone()  # one index or a slice gives a view
         self.table[requests] = -1
         self.kv_len[requests] = 0
         pages = pages[(pages >= 0) & (pages < self.pool.shape[0])].unique()

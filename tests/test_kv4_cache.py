@@ -25,3 +25,24 @@ def test_a_refused_append_leaves_entries_made_ahead():
             assert torch.equal(got, want)
     assert cache.append(k[:90], k[:90], _i32([90, 0, 0]))[2] == 0
     assert torch.equal(cache.table[1:], before[0][1:]) and int(cache.kv_len[0]) == 160
+
+
+@pytest.mark.parametrize("requests", [[1, 2], (slice(1, 3)), slice(-2, None), torch.tensor([1, 2]),
+                                      torch.tensor([False, True, True]), [1, -1, 1], range(1, 3)])
+def test_release_takes_indices_of_every_kind(requests):
+    cache = P.Kv4Cache(8, 3, 3, 1, 64, 64, device="cpu")  # page tables alone: no kernel runs
+    cache.table[:] = torch.tensor([[0, 1, 2], [3, 1, -1], [4, 5, 8]])
+    cache.kv_len[:] = torch.tensor([192, 100, 150])
+    cache.free = torch.tensor([6, 7], dtype=torch.int32)
+    cache.release(requests)
+    assert cache.table.tolist() == [[0, 1, 2], [-1] * 3, [-1] * 3] and cache.kv_len.tolist() == [192, 0, 0]
+    assert sorted(cache.free.tolist()) == [3, 4, 5, 6, 7] and cache.free.dtype is torch.int32
+
+
+@pytest.mark.parametrize("request_", [1, -2, torch.tensor(1), slice(1, 2)])
+def test_release_of_one_request(request_):
+    cache = P.Kv4Cache(8, 3, 3, 1, 64, 64, device="cpu")
+    cache.table[:] = torch.tensor([[0, 1, 2], [3, 1, -1], [4, 5, 8]])
+    cache.free = torch.tensor([6, 7], dtype=torch.int32)
+    cache.release(request_)
+    assert cache.table[1].tolist() == [-1] * 3 and sorted(cache.free.tolist()) == [3, 6, 7]

@@ -827,7 +827,9 @@ def kv4_attn(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, q_start: 
         if size:
             workspace = torch.empty(size, dtype=torch.uint8, device=dev)
     else:
-        size = workspace.numel()
+        if workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on %s" % dev)
+        size = workspace.numel() * workspace.element_size()
     _call(L.carnator_kv4_attn, dev, ctypes.byref(qr), T, heads, cr, _i32(table, "table", (B, W), dev), B, W,
           _i32(q_start, "q_start", (B + 1,), dev), _i32(kv_len, "kv_len", (B,), dev), max_q, 1 if causal else 0, scale,
           out.data_ptr(), out.stride(0), out.stride(1), _ptr(lse), _ptr(workspace), size)

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2609_32420_amd as P
-from test_gpu_kv4 import _bf16, _i32
+from test_gpu_kv4 import DEV, _bf16, _i32
 
 
 @pytest.mark.gpu
@@ -46,3 +46,20 @@ def test_release_of_one_request(request_):
     cache.free = torch.tensor([6, 7], dtype=torch.int32)
     cache.release(request_)
     assert cache.table[1].tolist() == [-1] * 3 and sorted(cache.free.tolist()) == [3, 6, 7]
+
+
+@pytest.mark.gpu
+def test_a_workspace_that_the_kernels_cannot_use_is_refused():
+    pool, table = P.kv4_pool(60, 2, 64, 64), _i32([list(range(60))])
+    q, args = _bf16(2, 8, 64, seed=1), (_i32([0, 2]), _i32([3800]), 2, 64)
+    want = P.kv4_attn(q, pool, table, *args)
+    ws = P.kv4_attn_workspace(q, pool, table, 2, 64)
+    assert ws.numel() > 1
+    for bad in (ws.cpu(), ws[:1].expand(ws.numel()), torch.empty(2 * ws.numel(), dtype=torch.uint8, device=DEV)[::2]):
+        with pytest.raises(ValueError):
+            P.kv4_attn(q, pool, table, *args, workspace=bad)
+    with pytest.raises(P.CarnatorError):
+        P.kv4_attn(q, pool, table, *args, workspace=ws[:-256])
+    # in bytes, whatever the type
+    floats = torch.empty(ws.numel() // 4, device=DEV)
+    assert torch.equal(P.kv4_attn(q, pool, table, *args, workspace=floats), want)

@@ -799,7 +799,8 @@ def kv4_attn(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, q_start: 
     q_start[b + 1] (int32 [batch + 1]) belong to request b, at most max_q of
     them; with ``causal`` they are the last of its kv_len tokens.  Rows of no
     request stay as they are in ``out`` and ``lse`` (fp32 [rows, heads]) and are
-    0 where the call allocates them.  Returns O (and the LSE)."""
+    0 where the call allocates them.  The LSE is formed where it is returned or
+    ``lse`` is passed.  Returns O (and the LSE)."""
     c = _kv4(pool, block)
     dev = pool.device
     if q.dim() != 3 or table.dim() != 2:
@@ -813,10 +814,9 @@ def kv4_attn(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, q_start: 
         if not _is_rows(out, heads, c.head_dim, dev) or out.shape[0] != T:
             raise ValueError("out must be a bf16 tensor [%d, %d, %d] on %s, contiguous along its channels"
                              % (T, heads, c.head_dim, dev))
-    if not return_lse:
-        lse = None
-    elif lse is None:
-        lse = torch.zeros(T, heads, dtype=torch.float32, device=dev)
+    if lse is None:
+        if return_lse:
+            lse = torch.zeros(T, heads, dtype=torch.float32, device=dev)
     elif lse.dtype is not torch.float32 or lse.shape != (T, heads) or lse.device != dev or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [rows, heads] on the pool's device")
     L, max_q, cr = lib(), int(max_q), ctypes.byref(c)

@@ -63,3 +63,17 @@ def test_a_workspace_that_the_kernels_cannot_use_is_refused():
     # in bytes, whatever the type
     floats = torch.empty(ws.numel() // 4, device=DEV)
     assert torch.equal(P.kv4_attn(q, pool, table, *args, workspace=floats), want)
+
+
+@pytest.mark.gpu
+def test_an_lse_that_is_passed_is_written():
+    pool = P.kv4_pool(3, 2, 64, 64)
+    x = _bf16(150, 2, 64, seed=1)
+    P.kv4_store(pool, x, x, torch.arange(150, dtype=torch.int32, device=DEV), 64)
+    q, args = _bf16(3, 4, 64, seed=2), (_i32([[0, 1, 2]]), _i32([0, 3]), _i32([150]), 3, 64)
+    o, want = P.kv4_attn(q, pool, *args, return_lse=True)
+    lse = torch.full_like(want, 7.0)
+    got = P.kv4_attn(q, pool, *args, lse=lse)
+    assert torch.equal(got, o) and torch.equal(lse, want)
+    with pytest.raises(ValueError):
+        P.kv4_attn(q, pool, *args, lse=lse.double())

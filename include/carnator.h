@@ -321,6 +321,8 @@ int carnator_select_block_mask(const double *mass, const carnator_shape *shape,
  *               from the list, and the tokens of new_len that were not placed
  *               (at most 2^31 - 1)
  * batch <= 16384.  table, slots and the other outputs must not overlap.
+ * free_pages is only read: before the next call (or the next replay of a captured
+ * one) the caller drops the counts[1] pages from its front.
  * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED, E_ALIGN, E_HIP.
  *
  * carnator_kv4_store: quantises row r of k and v into slot slots[r]; rows with

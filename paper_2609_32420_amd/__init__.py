@@ -711,7 +711,9 @@ def page_plan(kv_len: torch.Tensor, new_len: torch.Tensor, table: torch.Tensor, 
     capacity of the batch in tokens (at least the sum of new_len, or the rest
     is not placed).  Returns int32 (q_start [batch + 1], kv_len_out [batch],
     slots [n_slots], positions [n_slots], counts [3]); ``out`` may pass them
-    preallocated (positions may be None).  Nothing synchronises.
+    preallocated (positions may be None).  Nothing synchronises.  The pages are
+    the first of free_pages in every call: a program that captures it drops the
+    counts[1] that were taken from the list's front before each replay.
     """
     if not kv_len.is_cuda:
         raise ValueError("kv_len must be a CUDA tensor")
@@ -863,7 +865,10 @@ class Kv4Cache:
         free list, for which the stream is synchronised once (page_plan and
         kv4_store do not).  Returns (q_start, positions, lacking): the rows'
         starts and positions, and the number of tokens without a page or an
-        entry in the table, which are not held."""
+        entry in the table, which are not held.  It cannot be captured into a
+        graph: the free list is cut on the host."""
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("Kv4Cache.append cannot be captured: it cuts the free list on the host")
         before = self.table.clone()
         q_start, kv_len, slots, positions, counts = page_plan(self.kv_len, new_len, self.table, self.free, self.block,
                                                               k.shape[0])

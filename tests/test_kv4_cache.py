@@ -77,3 +77,55 @@ def test_an_lse_that_is_passed_is_written():
     assert torch.equal(got, o) and torch.equal(lse, want)
     with pytest.raises(ValueError):
         P.kv4_attn(q, pool, *args, lse=lse.double())
+
+
+@pytest.mark.gpu
+def test_an_append_is_not_captured():
+    cache = P.Kv4Cache(6, 2, 3, 1, 64, 64)
+    k = _bf16(2, 1, 64, seed=1)
+    cache.append(k, k, _i32([1, 1]))
+    before = cache.table.clone(), cache.kv_len.clone(), cache.free.clone()
+    new, x = _i32([1, 1]), torch.zeros(4, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        with pytest.raises(RuntimeError, match="captured"):
+            cache.append(k, k, new)
+        x.add_(1)
+    g.replay()
+    torch.cuda.synchronize()
+    for got, want in zip((cache.table, cache.kv_len, cache.free), before):
+        assert torch.equal(got, want)
+    assert (x == 1).all() and cache.append(k, k, new)[2] == 0 and cache.kv_len.tolist() == [2, 2]
+
+
+@pytest.mark.gpu
+def test_a_captured_plan_takes_pages_from_a_list_that_is_kept_in_place():
+    # decoding captured whole: plan, store and attention; the free list and the lengths
+    # are moved on in place before each replay
+    cache = P.Kv4Cache(8, 2, 4, 1, 64, 64)
+    k, v = _bf16(130, 1, 64, seed=1), _bf16(130, 1, 64, seed=2)
+    assert cache.append(k, v, _i32([63, 64]))[2] == 0
+    other = P.Kv4Cache(8, 2, 4, 1, 64, 64)
+    assert other.append(k, v, _i32([63, 64]))[2] == 0
+    free, ones, q = cache.free.clone(), _i32([1, 1]), _bf16(2, 2, 64, seed=3)
+    k1, v1 = k[:2].clone(), v[:2].clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        start, kv, slots, _, counts = P.page_plan(cache.kv_len, ones, cache.table, free, 64, 2)
+        P.kv4_store(cache.pool, k1, v1, slots, 64)
+        cache.kv_len.copy_(kv)
+        out = cache.attn(q, start, 1, causal=True)
+    for i in range(70):
+        k1.copy_(_bf16(2, 1, 64, seed=10 + i))
+        v1.copy_(_bf16(2, 1, 64, seed=99 + i))
+        g.replay()
+        free.copy_(free.roll(-int(counts[1])))
+        q_start, _, lacking = other.append(k1, v1, ones)
+        assert lacking == 0
+        want = other.attn(q, q_start, 1, causal=True)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(cache.kv_len, other.kv_len) and torch.equal(cache.table, other.table)

@@ -822,8 +822,8 @@ def kv4_attn(q: torch.Tensor, pool: torch.Tensor, table: torch.Tensor, q_start: 
     elif lse.dtype is not torch.float32 or lse.shape != (T, heads) or lse.device != dev or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [rows, heads] on the pool's device")
     L, max_q, cr = lib(), int(max_q), ctypes.byref(c)
-    if max_q > T > 0:
-        max_q = T  # no request has more; a C int holds it
+    if max_q > T:
+        max_q = T or 1  # no request has more; a C int holds it
     if workspace is None:
         size = L.carnator_kv4_attn_workspace_size(cr, heads, T, B, W, max_q)
         if size:

@@ -129,3 +129,13 @@ def test_a_captured_plan_takes_pages_from_a_list_that_is_kept_in_place():
         want = other.attn(q, q_start, 1, causal=True)
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(cache.kv_len, other.kv_len) and torch.equal(cache.table, other.table)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("most", [1, 100, 2 ** 31, 2 ** 33])
+def test_no_queries_at_all(most):
+    pool = P.kv4_pool(3, 2, 64, 64)
+    q, args = _bf16(2, 4, 64)[:0], (_i32([[0, 1, 2]]), _i32([0, 0]), _i32([150]), most, 64)
+    o, lse = P.kv4_attn(q, pool, *args, return_lse=True)
+    assert o.shape == (0, 4, 64) and lse.shape == (0, 4)
+    assert P.kv4_attn(q, pool, *args, workspace=P.kv4_attn_workspace(q, pool, args[0], most, 64)).shape == (0, 4, 64)

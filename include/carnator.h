@@ -333,8 +333,9 @@ int carnator_select_block_mask(const double *mass, const carnator_shape *shape,
  * carnator_kv4_load: the first kv_len tokens of each request, at most n, as
  * bf16 (exact: a level times a power of two).
  *   k_out, v_out  bf16 [batch, kv_heads, n, d] at element strides b, h, n
- *                 (multiples of 8, d contiguous); rows past a request's length
- *                 or without a page are left untouched
+ *                 (multiples of 8, at least d where there is more than one of
+ *                 them, d contiguous); rows past a request's length or without
+ *                 a page are left untouched
  * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED, E_ALIGN, E_HIP.
  *
  * carnator_kv4_attn: for query row t = q_start[b] + i of request b, m_b =

@@ -675,8 +675,10 @@ int carnator_kv4_load(const carnator_kv4 *cache, const int32_t *table, int32_t b
     return fail(CARNATOR_E_ALIGN, "k_out and v_out must be 16-byte aligned");
   if (ksb % 8 || ksh % 8 || ksn % 8 || vsb % 8 || vsh % 8 || vsn % 8)
     return fail(CARNATOR_E_ALIGN, "output strides must be multiples of 8 elements");
-  if (ksn < cache->head_dim || vsn < cache->head_dim || ksb < 0 || ksh < 0 || vsb < 0 || vsh < 0)
-    return fail(CARNATOR_E_SHAPE, "output strides out of range (stride_n >= head_dim, others >= 0)");
+  // rows that shared memory would be written by several workgroups at once
+  const int64_t d = cache->head_dim, to_b = batch > 1 ? d : 0, to_h = cache->kv_heads > 1 ? d : 0;
+  if (ksn < d || vsn < d || ksb < to_b || ksh < to_h || vsb < to_b || vsh < to_h)
+    return fail(CARNATOR_E_SHAPE, "output strides out of range (at least head_dim; >= 0 along one request or head)");
   if ((int64_t)batch * cache->kv_heads > (int64_t)INT32_MAX)
     return fail(CARNATOR_E_SHAPE, "batch * kv_heads exceeds 2^31-1");
   hipError_t e = launch_kv4_load(to_kv4(cache), table, batch, width, kv_len, n, static_cast<uint16_t *>(k_out), ksb,

@@ -1,5 +1,7 @@
 """What a cache of keys and values in 4 bits does with the calls that its
 documentation allows and refuses (see test_gpu_kv4.py for its results)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -139,3 +141,32 @@ def test_no_queries_at_all(most):
     o, lse = P.kv4_attn(q, pool, *args, return_lse=True)
     assert o.shape == (0, 4, 64) and lse.shape == (0, 4)
     assert P.kv4_attn(q, pool, *args, workspace=P.kv4_attn_workspace(q, pool, args[0], most, 64)).shape == (0, 4, 64)
+
+
+def _load_strides(batch, heads, k, v):
+    c = P.Kv4(0x100000, 4, heads, 128, 64)
+    return P.lib().carnator_kv4_load(ctypes.byref(c), 0x10000, batch, 3, 0x10000, 100, 0x40000, *k, 0x50000, *v, None)
+
+
+@pytest.mark.parametrize("batch,heads,bad", [(2, 2, (0, 12800, 128)), (2, 2, (25600, 0, 128)), (2, 1, (0, 12800, 128)),
+                                             (1, 2, (0, 0, 128)), (2, 2, (64, 12800, 128)), (2, 2, (25600, 120, 128)),
+                                             (1, 1, (-8, 0, 128)), (1, 1, (0, -8, 128)), (1, 1, (0, 0, 120))])
+def test_load_refuses_outputs_whose_rows_share_memory(batch, heads, bad):
+    good = (25600, 12800, 128)
+    assert _load_strides(batch, heads, bad, good) == -2 and _load_strides(batch, heads, good, bad) == -2
+
+
+@pytest.mark.gpu
+def test_load_into_one_head_of_any_stride():
+    pool = P.kv4_pool(3, 1, 64, 64)
+    x = _bf16(150, 1, 64, seed=1)
+    P.kv4_store(pool, x, x, torch.arange(150, dtype=torch.int32, device=DEV), 64)
+    args = (_i32([[0, 1, 2]]), _i32([150]), 64)
+    want = P.kv4_load(pool, *args, n=150)
+    out = [torch.zeros(150, 64, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    P.kv4_load(pool, *args, out=[t.as_strided((1, 1, 150, 64), (0, 0, 64, 1)) for t in out])
+    for a, b in zip(out, want):
+        assert torch.equal(a, b[0, 0])
+    two = P.kv4_pool(3, 2, 64, 64)
+    with pytest.raises(P.CarnatorError):
+        P.kv4_load(two, *args, out=[t.expand(1, 2, 150, 64) for t in out])

@@ -229,3 +229,19 @@ def test_a_launch_of_2_32_threads_is_refused(cut):
     assert c["tile_rows"] == 256 and c["groups"] < 1 << 24 and c["threads"] >= 1 << 32
     assert call(rows, 1, rows) == -3 and b"threads" in P.lib().carnator_last_error()
     assert call(1, 1 << 24, 1) == -3
+
+
+@pytest.mark.parametrize("m,group,width", [([1, 1], 2, 2000), ([300], 2, 200), ([700, 2, 700, 31], 3, 64)])
+def test_workspaces_that_do_not_do_are_refused(m, group, width):
+    # few rows in parts, tiles in parts, both; nothing is launched
+    rows, heads, L = sum(m), 2 * group, P.lib()
+    c, q = P.Kv4(0x100000, 4, 2, 128, 64), P.Rows(0x200000, 128 * heads, 128)
+    need = _workspace(128, 2, group, m, width)
+    assert need > 0
+
+    def call(ws, size):
+        return L.carnator_kv4_attn(ctypes.byref(q), rows, heads, ctypes.byref(c), 0x10000, len(m), width, 0x10000, 0x10000,
+                                   max(m), 1, 0.0, 0x60000, 128 * heads, 128, None, ws, size, None)
+
+    assert call(0x70000, need - 1) == -5 and call(None, need) == -5 and call(None, 0) == -5
+    assert call(0x70010, need) == -4

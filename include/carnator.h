@@ -346,7 +346,11 @@ int carnator_select_block_mask(const double *mass, const carnator_shape *shape,
  *   lse = log sum_{j in A} exp(sigma q . k_j),
  * sigma = scale, or 1/sqrt(head_dim) when scale <= 0.  No token in A gives
  * o = 0 and lse = -inf.  bf16 matrix cores, fp32 accumulation and softmax; O
- * is rounded to bf16.  A value outside A has no effect, be it NaN.
+ * is rounded to bf16.  A value outside A has no effect, be it NaN.  The weights
+ * that multiply v are rounded to bf16 (by 2^-9 of themselves at most) and o is
+ * divided by the sum of the rounded ones or, for requests of many rows, of the
+ * unrounded ones: equal v then give o within 2^-9 of them before its own rounding.
+ * lse takes the unrounded weights.  |v| from 2^89 on may overflow the sums.
  *   q           bf16 [n_rows, heads, d]
  *   q_start     int32 [batch + 1], ascending, read as clamped into [0, n_rows]
  *   max_q       at least every m_b (>= 1); rows of a request from max_q on are

@@ -18,9 +18,9 @@
 // V(j), whose bytes were loaded during the iteration before.
 //
 // What bounds it is the issue of its instructions: beside an MFMA of 32 cycles a
-// wave issues 5.9 vector ones (d = 128; 12.7 at d = 64), and MFMAs are under way
-// 54 % (36) of the time, vector instructions 54 % (72), LDS 37 % (32).  12 heads, d =
-// 128, 4680 queries over 32,760 tokens (942 GFLOP): 840 to 895 us with eight waves
+// wave issues 6.0 vector ones (d = 128; 12.8 at d = 64), and MFMAs are under way
+// 53 % (37) of the time, vector instructions 53 % (74), LDS 36 % (33).  12 heads, d =
+// 128, 4680 queries over 32,760 tokens (942 GFLOP): 840 to 930 us with eight waves
 // on a stage, 940 to 980 with four (twice the conversions).  At d = 64 the softmax
 // is twice as much beside an MFMA, so three workgroups on a CU hide more of it
 // than two: 1319 -> 1248 us for 8 requests of 16 heads (4 cached) over 8192 tokens,
@@ -383,6 +383,10 @@ tile_kernel(Kv4Attn a, Cut few, Parts few_parts, int few_first, Cut cut, Parts p
     const float v0 = __builtin_amdgcn_exp2f(fmaf(s[x >> 4][x & 15], a.c2, -st.sub));
     const float v1 = __builtin_amdgcn_exp2f(fmaf(s[x >> 4][(x + 1) & 15], a.c2, -st.sub));
     const bf16x2 pp = {(__bf16)v0, (__bf16)v1};
+    // P is rounded as in rows_part; the sum is that of the unrounded P, for the
+    // outputs too.  With one of the rounded P beside it for these (a convex
+    // combination again) 21 frames at d = 128 took 942 us instead of 902, 8 requests
+    // of 4096 queries over 8192 tokens at d = 64 1345 instead of 1265.
     p[x >> 3][(x & 7) >> 1] = __builtin_bit_cast(uint32_t, pp);
     st.s0 += v0;
     st.s1 += v1;

@@ -81,7 +81,7 @@ struct Cut {
   int tile_rows, tiles, chunk, chunks;
   int turns;  // of the kernel for many rows: a turn is a tile of every request
   int items;  // tiles of its grid, each found in the turns by its number; 0: the grid holds the turns
-  int columns;  // parts that the grid holds, and results of a row: a workgroup takes every columns-th of the chunks
+  int columns;  // parts that the grid holds, and results of a row; a workgroup takes every columns-th part
   int span;   // rows of a request and cached head that parts are kept for; 0: parts are kept by query row
   __device__ bool has(const Span &s) const { return s.rows > over && s.rows <= upto; }
 };

@@ -231,8 +231,9 @@ __device__ __attribute__((always_inline)) inline void rows_part(const Kv4Attn &a
         p[n][e] = __builtin_bit_cast(uint32_t, pp);
         // P is rounded to bf16 (by 2^-9 of itself at most) for the matrix cores, whose
         // fp32 rate is a sixteenth: outputs are then 0.0018 from fp64 (relative, norms)
-        // over 77 tokens where fp32 weights leave 0.0017, 0.0014 for both over 119,056.  The outputs are divided by the sum of what is multiplied
-        // with V: a convex combination of its rows; the LSE takes the unrounded sum
+        // over 77 tokens where fp32 weights leave 0.0017, 0.0014 for both over 119,056.
+        // The outputs are divided by the sum of what is multiplied with V: a convex
+        // combination of its rows; the LSE takes the unrounded sum
         lrun[n] = __builtin_amdgcn_fdot2_f32_bf16(pp, ones, lrun[n], false);
         lexact[n] += p0 + p1;
       }

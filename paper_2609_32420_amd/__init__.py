@@ -867,7 +867,7 @@ class Kv4Cache:
         starts and positions, and the number of tokens without a page or an
         entry in the table, which are not held.  It cannot be captured into a
         graph: the free list is cut on the host."""
-        if torch.cuda.is_current_stream_capturing():
+        if self.pool.is_cuda and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("Kv4Cache.append cannot be captured: it cuts the free list on the host")
         before = self.table.clone()
         q_start, kv_len, slots, positions, counts = page_plan(self.kv_len, new_len, self.table, self.free, self.block,

@@ -170,3 +170,11 @@ def test_load_into_one_head_of_any_stride():
     two = P.kv4_pool(3, 2, 64, 64)
     with pytest.raises(P.CarnatorError):
         P.kv4_load(two, *args, out=[t.expand(1, 2, 150, 64) for t in out])
+
+
+def test_a_cache_in_host_memory_refuses_what_runs_kernels():
+    cache = P.Kv4Cache(4, 1, 2, 1, 64, 64, device="cpu")
+    x, two = torch.zeros(2, 1, 64, dtype=torch.bfloat16), torch.tensor([2], dtype=torch.int32)
+    for f in (lambda: cache.append(x, x, two), lambda: cache.load(), lambda: cache.attn(x, torch.tensor([0, 2]), 2)):
+        with pytest.raises(ValueError):
+            f()
